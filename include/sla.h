@@ -180,6 +180,67 @@ int sla_aggregate_ws_bytes(const sla_params* p, int method, uint64_t* bytes);
 int sla_aggregate_states(const sla_params* p, int method, const void* luts, const void* h, void* outH,
                          float* outZ, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- softmax attention of the layers around SLA: cross attention, layers kept dense, causal layers with K, V heads
+ * that several query heads share, text encoders with a learned position bias, generation over a cache.
+ *
+ * Per sequence b and query head h (K, V head h / (H / Hkv)), query n at position n + q0(b), key at position kp:
+ *   S = scale Q K^T + bias;  L = log sum exp S and P = exp(S - L) over the allowed keys;  O = P V
+ *   dV = P^T dO;  dS = P (dO V^T - rowsum(dO O));  dQ = scale dS K;  dK = scale dS^T Q (dK, dV: summed over the query
+ *   heads of their head);  dtable[u][h] = sum of dS over the pairs (of all sequences) in bucket u
+ * The keys are the Np rows of a prefix that all sequences share (its K, V are fetched once for all of them), at positions
+ * 0 .. Np - 1, and behind it the sequence's own first k_len[b] rows, at positions Np ...  A key is allowed where it
+ * exists and, with `causal`, kp <= n + q0(b).  Queries n >= q_len[b] and those without an allowed key are empty rows:
+ * O = 0, L = -inf, no gradients.  Rows of Q and dO behind q_len[b], and of K and V behind k_len[b], are not read; those
+ * of dQ, dK, dV are written as zeros.  (Keys that only `causal` hides have to be finite: they meet a probability of
+ * zero in a product.) */
+
+/* Buckets of the distance r = kp - (n + q0(b)).  With m = |r| (two_sided) or max(-r, 0): bucket = number of borders
+ * <= m, plus n_buckets / 2 where two_sided and r > 0.  n_buckets = 0: no bias.  A side has n_buckets (two_sided:
+ * n_buckets / 2) buckets, at most 64, and one border less; borders ascend from 1 at least to SLA_ATTN_MAX_DISTANCE. */
+enum { SLA_ATTN_BORDERS = 63, SLA_ATTN_MAX_DISTANCE = 1024 };
+typedef struct sla_buckets {
+  int32_t n_buckets, two_sided;
+  int32_t borders[SLA_ATTN_BORDERS];
+} sla_buckets;
+
+typedef struct sla_attn_params {
+  int32_t B, H, Hkv;    /* sequences, query heads, K and V heads (a divisor of H)            */
+  int32_t Nq, Nk, Np;   /* rows of Q; of K and V (0 allowed); of the prefix (0: none)        */
+  int32_t d, dtype;     /* 64 or 128; SLA_F32 or SLA_BF16                                    */
+  int32_t causal;
+  int32_t q_pos;        /* q0(b) = q_pos, or with q_from_end Np + k_len[b] + q_pos (the      */
+  int32_t q_from_end;   /* newest Nq tokens of every sequence: q_pos = -Nq)                  */
+  int32_t table_dtype;  /* of the bias table and its gradient: SLA_F32 or SLA_BF16           */
+  float scale;          /* of the scores, > 0                                                */
+  sla_buckets buckets;
+} sla_attn_params;
+
+/* Element (b, h, n, c) of a tensor sits b stride_b + h stride_h + n stride_n + c elements behind data (of the prefix:
+ * h stride_h + n stride_n + c).  Strides are multiples of 16 bytes, not negative, stride_n at least d and at most 16 MB; those
+ * of an axis of length one are not used.  Rows of O, dQ, dK, dV must not overlap. */
+typedef struct sla_tensor {
+  void* data;
+  int64_t stride_b, stride_h, stride_n;
+} sla_tensor;
+
+/* Bytes of workspace of the two calls below (backward: 0 with a prefix, which has no backward pass).  Host-only. */
+int sla_attn_sizes(const sla_attn_params* p, uint64_t* forward_bytes, uint64_t* backward_bytes);
+
+/* Kp, Vp: the prefix, or NULL where Np = 0.  table: table_dtype [n_buckets, H], or NULL without buckets.  q_len, k_len:
+ * int32 [B] or NULL (all Nq, all Nk); values outside the tensor are cut to it.  O (out); L: float [B, H, Nq] (out),
+ * or NULL.  workspace: >= forward_bytes (may be NULL when that is 0). */
+int sla_attn_forward(const sla_attn_params* p, const sla_tensor* Q, const sla_tensor* K, const sla_tensor* V,
+                     const sla_tensor* Kp, const sla_tensor* Vp, const void* table, const int32_t* q_len,
+                     const int32_t* k_len, const sla_tensor* O, float* L, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* O, L: as written by sla_attn_forward with the same inputs (Np = 0).  dQ, dK, dV (out); dtable: table_dtype
+ * [n_buckets, H] (out), or NULL.  A head of any of the tensors spans less than 2^31 bytes (SLA_EUNSUPPORTED). */
+int sla_attn_backward(const sla_attn_params* p, const sla_tensor* Q, const sla_tensor* K, const sla_tensor* V,
+                      const sla_tensor* O, const sla_tensor* dO, const float* L, const void* table,
+                      const int32_t* q_len, const int32_t* k_len, const sla_tensor* dQ, const sla_tensor* dK,
+                      const sla_tensor* dV, void* dtable, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Optional per-kernel timing for benchmarks.  While enabled, each kernel the library
  * launches is bracketed by a pair of HIP events on the caller's stream.
  * sla_profile_read waits for the recorded events, writes one line "name count total_ms"

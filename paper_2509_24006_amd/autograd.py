@@ -6,6 +6,14 @@ runs sla_build_mask + sla_forward and records sla_backward; every step is a kern
 libsla_hip.so, this module only keeps the buffers alive between the two passes.  The mask is a
 constant of the graph (no gradient flows into the block scores); a mask built once can be passed
 back in through `mask=` and reused, e.g. across the steps of a diffusion sampler.
+
+The layers around it:
+
+    O = dense_attention(Q, K, V, causal=..., k_len=..., table=..., buckets=position_buckets(32, 128))
+    O = cached_attention(Q, K_cache, V_cache, k_len=lengths, prefix=(K_prompt, V_prompt))
+
+softmax attention with gradients (cross attention, dense or causal layers, shared K, V heads, learned position
+bias), and its serving form for the newest tokens of every sequence of a batch.
 """
 from __future__ import annotations
 
@@ -14,6 +22,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import binding as sla
+from .binding import position_buckets  # noqa: F401  (the buckets of dense_attention's and cached_attention's bias)
 
 
 class _SLAFunction(torch.autograd.Function):
@@ -74,3 +83,86 @@ def sla_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, W: torch.Te
     grad = torch.is_grad_enabled() and any(
         getattr(t, "requires_grad", False) for t in (Q, K, V, W))
     return _SLAFunction.apply(Q, K, V, W, p, Mc, luts, grad)
+
+
+class _AttnFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, Q, K, V, table, p, q_len, k_len, token_major):
+        O, L = sla.sla_attn_forward(p, Q, K, V, table, q_len, k_len, token_major=token_major)
+        ctx.p, ctx.token_major = p, token_major
+        ctx.save_for_backward(Q, K, V, table, O, L, q_len, k_len)
+        return O
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dO):
+        Q, K, V, table, O, L, q_len, k_len = ctx.saved_tensors
+        grads = sla.sla_attn_backward(ctx.p, Q, K, V, O, _laid_out(dO, ctx.token_major), L, table, q_len, k_len, ctx.token_major)
+        return (*grads, None, None, None, None)
+
+
+def _laid_out(t: torch.Tensor, token_major: bool) -> torch.Tensor:
+    """The tensor itself where the library reads its strides (features contiguous, everything at multiples of 16
+    bytes, rows next to or apart from each other), else a copy of it."""
+    s, n, q, rows = t.stride(), t.shape, 16 // t.element_size(), t.dim() - (3 if token_major else 2)
+    fits = s[-1] == 1 and t.data_ptr() % 16 == 0
+    for i in range(t.dim() - 1):
+        if n[i] > 1:
+            fits = fits and s[i] % q == 0 and (i != rows or n[-1] <= s[i] <= (1 << 24) // t.element_size())
+    return t if fits else t.contiguous()
+
+
+def _attn_params(Q, K, causal, scale, table, buckets, token_major, prefix_rows=0, from_end=False):
+    if Q.dim() != 4 or K.dim() != 4:
+        raise sla.SLAError("Q, K, V: expected tensors of four dimensions")
+    if (table is None) != (buckets is None):
+        raise sla.SLAError("table: a bias takes both, the buckets and the table")
+    B, H, Nq, d = Q.shape if not token_major else (Q.shape[0], Q.shape[2], Q.shape[1], Q.shape[3])
+    Hkv, Nk = (K.shape[2], K.shape[1]) if token_major else (K.shape[1], K.shape[2])
+    return sla.make_attn_params(B, H, Hkv, Nq, Nk, d, Q.dtype, causal, scale, prefix_rows,
+                                -Nq if from_end else Nk - Nq, from_end, buckets,
+                                torch.float32 if table is None else table.dtype)
+
+
+def dense_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: bool = False,
+                    scale: Optional[float] = None, q_len: Optional[torch.Tensor] = None,
+                    k_len: Optional[torch.Tensor] = None, table: Optional[torch.Tensor] = None,
+                    buckets: Optional[sla.sla_buckets] = None, token_major: bool = False) -> torch.Tensor:
+    """O = softmax(scale Q K^T + bias) V with gradients to Q, K, V and the bias table.
+
+    Q [B,H,Nq,d], K, V [B,Hkv,Nk,d] with Hkv a divisor of H (query head h reads K, V head h // (H // Hkv)), or
+    with token_major [B,Nq,H,d], [B,Nk,Hkv,d]; bf16 or float32, d 64 or 128; O as Q.  scale: 1 / sqrt(d) unless given.
+    causal: query n sees the keys up to n + Nk - Nq.  q_len, k_len (int32 [B], on the device): valid queries and
+    keys of every sequence; what lies behind them is not read, and comes back as zeros.  table [n_buckets,H] (float32
+    or bf16) with buckets = position_buckets(...): table[bucket(key position - query position), head] is added
+    to the scaled scores."""
+    Q, K, V = (_laid_out(t, token_major) for t in (Q, K, V))
+    p = _attn_params(Q, K, causal, scale, table, buckets, token_major)
+    if table is not None and not table.is_contiguous():
+        table = table.contiguous()
+    if torch.is_grad_enabled() and any(getattr(t, "requires_grad", False) for t in (Q, K, V, table)):
+        return _AttnFunction.apply(Q, K, V, table, p, q_len, k_len, token_major)
+    return sla.sla_attn_forward(p, Q, K, V, table, q_len, k_len, token_major=token_major, need_L=False)[0]
+
+
+def cached_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, k_len: Optional[torch.Tensor] = None,
+                     prefix: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, causal: bool = True,
+                     scale: Optional[float] = None, table: Optional[torch.Tensor] = None,
+                     buckets: Optional[sla.sla_buckets] = None, token_major: bool = False) -> torch.Tensor:
+    """Attention of the newest Nq tokens of every sequence over its cache, without gradients.
+
+    K, V [B,Hkv,Nk,d] (token_major: [B,Nk,Hkv,d]) are the caches, the new tokens' rows among them; k_len (int32 [B]): rows
+    that are in use, all unless given.  prefix = (K, V) [Hkv,Np,d] (token_major: [Np,Hkv,d]): rows that come before
+    every sequence's own, fetched once for the whole batch.  The queries are the last Nq tokens in use (causal among
+    themselves); a sequence with fewer than Nq of them, behind no prefix, has rows without a key, which are zeros."""
+    with torch.no_grad():
+        Q, K, V = (_laid_out(t, token_major) for t in (Q, K, V))
+        if prefix is not None:
+            prefix = tuple(_laid_out(t, token_major) for t in prefix)
+        Np = 0 if prefix is None else prefix[0].shape[0 if token_major else 1]
+        if prefix is not None and Np == 0:
+            prefix = None
+        p = _attn_params(Q, K, causal, scale, table, buckets, token_major, Np, True)
+        if table is not None and not table.is_contiguous():
+            table = table.contiguous()
+        return sla.sla_attn_forward(p, Q, K, V, table, None, k_len, prefix, token_major, need_L=False)[0]

@@ -21,8 +21,10 @@ SLA_PHI_SOFTMAX, SLA_PHI_ELU1 = 0, 1
 SLA_BHND, SLA_BNHD, SLA_STRIDED = 0, 1, 2
 SLA_AGG_GEMM, SLA_AGG_ADD, SLA_AGG_PREAGG, SLA_AGG_FOUR_RUSSIANS = 0, 1, 2, 3
 SLA_STATIC_WS_BYTES = 32 << 20
+SLA_ATTN_BORDERS, SLA_ATTN_MAX_DISTANCE = 63, 1024
 EXPORTS = ("sla_sizes", "sla_build_mask", "sla_build_mask_static", "sla_classify_scores", "sla_forward", "sla_mask_forward", "sla_backward", "sla_backward_typed",
            "sla_aggregate_ws_bytes", "sla_aggregate_states", "sla_wide_query_tiles",
+           "sla_attn_sizes", "sla_attn_forward", "sla_attn_backward",
            "sla_profile_enable", "sla_profile_read", "sla_profile_mfma_peak", "sla_profile_dq_atomics", "sla_strerror")
 
 
@@ -41,6 +43,21 @@ class sla_sizes_t(ctypes.Structure):
                     "saved_bytes", "saved_Os", "saved_Ol", "saved_L", "saved_HZ", "saved_Z",
                     "ws_mask_bytes", "ws_mask_qbar", "ws_mask_kbar", "ws_mask_scores",
                     "ws_forward_bytes", "ws_backward_bytes")]
+
+
+class sla_buckets(ctypes.Structure):
+    _fields_ = [("n_buckets", ctypes.c_int32), ("two_sided", ctypes.c_int32), ("borders", ctypes.c_int32 * SLA_ATTN_BORDERS)]
+
+
+class sla_attn_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "Hkv", "Nq", "Nk", "Np", "d", "dtype", "causal", "q_pos",
+                                              "q_from_end", "table_dtype")] + [("scale", ctypes.c_float),
+                                                                               ("buckets", sla_buckets)]
+
+
+class sla_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64)]
 
 
 class SLAError(RuntimeError):
@@ -70,6 +87,10 @@ def lib() -> ctypes.CDLL:
         L.sla_backward_typed.argtypes = [pp] + [vp] * 12 + [ctypes.c_int, vp, sz, vp]
         L.sla_aggregate_ws_bytes.argtypes = [pp, ctypes.c_int, ctypes.POINTER(ctypes.c_uint64)]
         L.sla_aggregate_states.argtypes = [pp, ctypes.c_int, vp, vp, vp, vp, vp, sz, vp]
+        ap, tp, u64 = ctypes.POINTER(sla_attn_params), ctypes.POINTER(sla_tensor), ctypes.POINTER(ctypes.c_uint64)
+        L.sla_attn_sizes.argtypes = [ap, u64, u64]
+        L.sla_attn_forward.argtypes = [ap] + [tp] * 5 + [vp] * 3 + [tp, vp, vp, sz, vp]
+        L.sla_attn_backward.argtypes = [ap] + [tp] * 5 + [vp] * 4 + [tp] * 3 + [vp, vp, sz, vp]
         L.sla_profile_enable.argtypes = [ctypes.c_int]
         L.sla_wide_query_tiles.argtypes = [ctypes.c_int]
         L.sla_profile_read.argtypes = [ctypes.c_char_p, sz]
@@ -335,6 +356,171 @@ def sla_aggregate_states(p: sla_params, method: int, luts: torch.Tensor, h: torc
                                       _ptr(ws), ws.numel() if ws is not None else 0, _stream()),
            "sla_aggregate_states")
     return out
+
+
+# ---- softmax attention (cross attention, dense and causal layers, position bias, generation over a cache)
+
+def position_buckets(n_buckets: int, max_distance: int, two_sided: bool = True) -> sla_buckets:
+    """Buckets of the distance key position - query position for a learned bias: of the buckets of a side (with
+    two_sided half of them are for keys behind the query, else such keys share bucket 0) the first half holds one
+    distance each, and the others grow by a constant factor up to max_distance, beyond which all distances
+    share the last one.  The borders e (max_distance / e)^(k / m) are rounded up in whole numbers."""
+    side = n_buckets // 2 if two_sided else n_buckets
+    e = side // 2
+    if n_buckets != side * (2 if two_sided else 1) or not 2 <= side <= SLA_ATTN_BORDERS + 1:
+        raise SLAError(f"n_buckets: expected 2 to {SLA_ATTN_BORDERS + 1} buckets a side, got {n_buckets}"
+                       f"{' for two sides' if two_sided else ''}")
+    if not e < max_distance <= SLA_ATTN_MAX_DISTANCE:
+        raise SLAError(f"max_distance: expected {e + 1} to {SLA_ATTN_MAX_DISTANCE}, got {max_distance}")
+    borders, m = list(range(1, e + 1)), side - e
+    for k in range(1, m):
+        n = borders[-1]
+        while n ** m < max_distance ** k * e ** (m - k):
+            n += 1
+        borders.append(n)
+    return sla_buckets(n_buckets, int(two_sided), (ctypes.c_int32 * SLA_ATTN_BORDERS)(*borders))
+
+
+def make_attn_params(B: int, H: int, Hkv: int, Nq: int, Nk: int, d: int, dtype: torch.dtype, causal: bool = False,
+                     scale: Optional[float] = None, Np: int = 0, q_pos: int = 0, q_from_end: bool = False,
+                     buckets: Optional[sla_buckets] = None, table_dtype: torch.dtype = torch.float32) -> sla_attn_params:
+    """scale: 1 / sqrt(d) unless given.  q_pos: position of the first query, or with q_from_end its position
+    counted from the end of the sequence's valid keys (-Nq: the newest Nq tokens).  buckets: of the position bias."""
+    code = {torch.float32: SLA_F32, torch.bfloat16: SLA_BF16}
+    for t in (dtype, table_dtype):
+        if t not in code:
+            raise SLAError(f"expected float32 or bfloat16 tensors, got {t}")
+    p = sla_attn_params(B, H, Hkv, Nq, Nk, Np, d, code[dtype], int(causal), q_pos, int(q_from_end), code[table_dtype],
+                        d ** -0.5 if scale is None else scale)
+    if buckets is not None:
+        p.buckets = buckets
+    return p
+
+
+def sla_attn_sizes(p: sla_attn_params) -> Tuple[int, int]:
+    """bytes of workspace of the forward and of the backward call"""
+    f, b = ctypes.c_uint64(), ctypes.c_uint64()
+    _check(lib().sla_attn_sizes(ctypes.byref(p), ctypes.byref(f), ctypes.byref(b)), "sla_attn_sizes")
+    return f.value, b.value
+
+
+def _rows(t: torch.Tensor, p: sla_attn_params, heads: int, n: int, token_major: bool, what: str, like=None):
+    """Q, K, V, O, dO, dQ, dK, dV as the C ABI takes them"""
+    want = (p.B, n, heads, p.d) if token_major else (p.B, heads, n, p.d)
+    dt = torch.float32 if p.dtype == SLA_F32 else torch.bfloat16
+    if (not isinstance(t, torch.Tensor) or t.dtype != dt or tuple(t.shape) != want or t.stride(3) != 1 or not t.is_cuda
+            or (like is not None and t.device != like.device)):
+        raise SLAError(f"{what}: expected a {dt} device tensor of shape {want} with contiguous features, got "
+                       f"{getattr(t, 'dtype', type(t))} {tuple(getattr(t, 'shape', ()))} on {getattr(t, 'device', None)}")
+    s = t.stride()
+    return sla_tensor(t.data_ptr(), s[0], s[2 if token_major else 1], s[1 if token_major else 2])
+
+
+def _prefix(t: torch.Tensor, p: sla_attn_params, token_major: bool, what: str, like):
+    want = (p.Np, p.Hkv, p.d) if token_major else (p.Hkv, p.Np, p.d)
+    if (not isinstance(t, torch.Tensor) or t.dtype != like.dtype or tuple(t.shape) != want or t.stride(2) != 1
+            or t.device != like.device):
+        raise SLAError(f"{what}: expected a {like.dtype} tensor of shape {want} on {like.device}")
+    s = t.stride()
+    return sla_tensor(t.data_ptr(), 0, s[1 if token_major else 0], s[0 if token_major else 1])
+
+
+def _flat(t, shape, dtype, what, like):
+    _packed(t, shape, dtype, what)
+    if t.device != like.device:
+        raise SLAError(f"{what}: expected a tensor on {like.device}, got one on {t.device}")
+    return t
+
+
+def _attn_extras(p, table, q_len, k_len, like):
+    if (table is not None) != (p.buckets.n_buckets > 0):
+        raise SLAError("table: a bias takes both, the buckets and the table")
+    if table is not None:
+        _flat(table, (p.buckets.n_buckets, p.H), torch.float32 if p.table_dtype == SLA_F32 else torch.bfloat16, "table", like)
+    for n, t in (("q_len", q_len), ("k_len", k_len)):
+        if t is not None:
+            _flat(t, (p.B,), torch.int32, n, like)
+
+
+def _out_rows(p, heads, n, token_major, like):
+    return torch.empty((p.B, n, heads, p.d) if token_major else (p.B, heads, n, p.d), dtype=like.dtype, device=like.device)
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
+
+
+def sla_attn_forward(p: sla_attn_params, Q, K, V, table=None, q_len=None, k_len=None, prefix=None, token_major: bool = False,
+                     O: Optional[torch.Tensor] = None, L: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, need_L: bool = True
+                     ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Returns (O, L); L float32 [B,H,Nq] is None when need_L is False.  Q [B,H,Nq,d], K, V [B,Hkv,Nk,d], prefix = (K, V)
+    [Hkv,Np,d], or with token_major [B,Nq,H,d], [B,Nk,Hkv,d], [Np,Hkv,d]: views with contiguous features.  Runs on the
+    current stream of Q's device."""
+    Kp, Vp = (None, None) if prefix is None else prefix
+    token_major = bool(token_major)
+    r = _host_calls().attn_forward(ctypes.addressof(p), Q, K, V, Kp, Vp, table, q_len, k_len, token_major, O, L, workspace,
+                                   bool(need_L))
+    if type(r) is tuple:
+        return r
+    if r is not None:
+        _check(r, "sla_attn_forward")
+    need = sla_attn_sizes(p)[0]
+    q = _rows(Q, p, p.H, p.Nq, token_major, "Q")
+    k, v = (_rows(t, p, p.Hkv, p.Nk, token_major, n, Q) for n, t in (("K", K), ("V", V)))
+    if (prefix is not None) != (p.Np > 0):
+        raise SLAError("prefix: the params state another number of rows")
+    kp, vp = (None, None) if prefix is None else (ctypes.byref(_prefix(t, p, token_major, "prefix", Q)) for t in prefix)
+    _attn_extras(p, table, q_len, k_len, Q)
+    if O is None:
+        O = _out_rows(p, p.H, p.Nq, token_major, Q)
+    if L is None and need_L:
+        L = torch.empty((p.B, p.H, p.Nq), dtype=torch.float32, device=Q.device)
+    if L is not None:
+        _flat(L, (p.B, p.H, p.Nq), torch.float32, "L", Q)
+    ws = workspace if workspace is not None else _buf(need, Q.device)
+    _flat(_bytes(ws, need, "workspace"), ws.shape, torch.uint8, "workspace", Q)
+    with torch.cuda.device(Q.device):
+        _check(lib().sla_attn_forward(ctypes.byref(p), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v), kp, vp,
+                                      _ptr(table), _ptr(q_len), _ptr(k_len),
+                                      ctypes.byref(_rows(O, p, p.H, p.Nq, token_major, "O", Q)), _ptr(L), _ptr(ws),
+                                      ws.numel(), _stream_of(Q)), "sla_attn_forward")
+    return O, L
+
+
+def sla_attn_backward(p: sla_attn_params, Q, K, V, O, dO, L, table=None, q_len=None, k_len=None, token_major: bool = False,
+                      workspace: Optional[torch.Tensor] = None, out=None):
+    """Returns (dQ, dK, dV, dtable); dtable, in the table's type, is None without a bias.  out: tensors for the four."""
+    token_major = bool(token_major)
+    r = _host_calls().attn_backward(ctypes.addressof(p), Q, K, V, O, dO, L, table, q_len, k_len, token_major, workspace,
+                                    *((None,) * 4 if out is None else out))
+    if type(r) is tuple:
+        return r
+    if r is not None:
+        _check(r, "sla_attn_backward")
+    if p.Np:
+        raise SLAError("prefix: there is no backward pass behind one")
+    need = sla_attn_sizes(p)[1]
+    rows = lambda t, heads, n, what: ctypes.byref(_rows(t, p, heads, n, token_major, what, Q))
+    q, k, v = rows(Q, p.H, p.Nq, "Q"), rows(K, p.Hkv, p.Nk, "K"), rows(V, p.Hkv, p.Nk, "V")
+    o, do = rows(O, p.H, p.Nq, "O"), rows(dO, p.H, p.Nq, "dO")
+    _flat(L, (p.B, p.H, p.Nq), torch.float32, "L", Q)
+    _attn_extras(p, table, q_len, k_len, Q)
+    dQ, dK, dV, dT = (None,) * 4 if out is None else out
+    dQ = _out_rows(p, p.H, p.Nq, token_major, Q) if dQ is None else dQ
+    dK = _out_rows(p, p.Hkv, p.Nk, token_major, Q) if dK is None else dK
+    dV = _out_rows(p, p.Hkv, p.Nk, token_major, Q) if dV is None else dV
+    if dT is not None and table is None:
+        raise SLAError("dtable: there is no table")
+    if table is not None:
+        dT = torch.empty_like(table) if dT is None else _flat(dT, tuple(table.shape), table.dtype, "dtable", Q)
+    ws = workspace if workspace is not None else _buf(need, Q.device)
+    _flat(_bytes(ws, need, "workspace"), ws.shape, torch.uint8, "workspace", Q)
+    with torch.cuda.device(Q.device):
+        _check(lib().sla_attn_backward(ctypes.byref(p), q, k, v, o, do, _ptr(L), _ptr(table), _ptr(q_len), _ptr(k_len),
+                                       rows(dQ, p.H, p.Nq, "dQ"), rows(dK, p.Hkv, p.Nk, "dK"), rows(dV, p.Hkv, p.Nk, "dV"),
+                                       _ptr(dT), _ptr(ws), ws.numel(), _stream_of(Q)), "sla_attn_backward")
+    return dQ, dK, dV, dT
 
 
 def sla_wide_query_tiles(on: bool) -> None:

@@ -12,6 +12,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 
 #include "../../include/sla.h"
 
@@ -251,11 +252,168 @@ PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- softmax attention
+
+bool stream_of(const at::Tensor& t, void** out) {   // the current stream of the tensor's device
+  PyObject* dev = PyLong_FromLong(t.get_device());
+  if (!dev) return false;
+  PyObject* st = PyObject_CallFunctionObjArgs(g_stream, dev, nullptr);
+  Py_DECREF(dev);
+  if (!st) return false;
+  *out = PyLong_AsVoidPtr(st);
+  Py_DECREF(st);
+  return !PyErr_Occurred();
+}
+
+struct AttnCall {
+  const sla_attn_params* p;
+  uint64_t fwd, bwd;
+  at::ScalarType dt, tt;
+  bool token;   // [B, N, H, d] tensors
+  at::Device dev = at::kCPU;
+
+  bool open(PyObject* addr, PyObject* token_major, const at::Tensor* Q) {
+    p = static_cast<const sla_attn_params*>(PyLong_AsVoidPtr(addr));
+    if (!p || !Q || !Q->is_cuda() || sla_attn_sizes(p, &fwd, &bwd) != SLA_OK) return false;
+    dt = p->dtype == SLA_F32 ? at::kFloat : at::kBFloat16;
+    tt = p->table_dtype == SLA_F32 ? at::kFloat : at::kBFloat16;
+    token = token_major == Py_True;
+    dev = Q->device();
+    return true;
+  }
+  bool here(const at::Tensor* t, at::ScalarType type) const { return t && t->device() == dev && t->scalar_type() == type; }
+  bool rows(const at::Tensor* t, int heads, int n, sla_tensor* out) const {
+    if (!here(t, dt) || t->dim() != 4) return false;
+    const auto s = t->sizes(), st = t->strides();
+    const int hx = token ? 2 : 1, nx = token ? 1 : 2;
+    if (s[0] != p->B || s[hx] != heads || s[nx] != n || s[3] != p->d || st[3] != 1) return false;
+    *out = sla_tensor{t->data_ptr(), st[0], st[hx], st[nx]};
+    return true;
+  }
+  bool prefix(const at::Tensor* t, sla_tensor* out) const {
+    if (!here(t, dt) || t->dim() != 3) return false;
+    const auto s = t->sizes(), st = t->strides();
+    const int hx = token ? 1 : 0, nx = token ? 0 : 1;
+    if (s[hx] != p->Hkv || s[nx] != p->Np || s[2] != p->d || st[2] != 1) return false;
+    *out = sla_tensor{t->data_ptr(), 0, st[hx], st[nx]};
+    return true;
+  }
+  bool flat(const at::Tensor* t, at::IntArrayRef shape, at::ScalarType type) const {
+    return here(t, type) && t->sizes() == shape && t->is_contiguous();
+  }
+  // lengths [B] and the table: absent (None) or as stated
+  bool lengths(PyObject* o, const int32_t** out) const {
+    *out = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = plain(o);
+    if (!flat(t, {p->B}, at::kInt)) return false;
+    *out = t->const_data_ptr<int32_t>();
+    return true;
+  }
+  bool table(PyObject* o, const void** out) const {
+    *out = nullptr;
+    if (o == Py_None) return p->buckets.n_buckets == 0;
+    const at::Tensor* t = plain(o);
+    if (!flat(t, {p->buckets.n_buckets, p->H}, tt)) return false;
+    *out = t->const_data_ptr();
+    return true;
+  }
+  at::Tensor fresh(const at::Tensor& like, int heads, int n, sla_tensor* out) const {
+    const int64_t B = p->B, h = heads, m = n, d = p->d;
+    at::Tensor t = at::empty(token ? at::IntArrayRef{B, m, h, d} : at::IntArrayRef{B, h, m, d},
+                             like.options().requires_grad(false));
+    rows(&t, heads, n, out);
+    return t;
+  }
+};
+
+// attn_forward(params address, Q, K, V, prefix K, prefix V, table, q_len, k_len, token_major, O, L, workspace, need_L)
+// -> (O, L or None)
+PyObject* attn_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  AttnCall c;
+  if (n != 14) Py_RETURN_NONE;
+  const at::Tensor *Q = plain(a[1]), *K = plain(a[2]), *V = plain(a[3]);
+  sla_tensor q, k, v, kp, vp, o;
+  const void* table;
+  const int32_t *q_len, *k_len;
+  Slot O(a[10]), L(a[11]), ws(a[12]);
+  if (!c.open(a[0], a[9], Q)) Py_RETURN_NONE;
+  const sla_attn_params& p = *c.p;
+  if (!c.rows(Q, p.H, p.Nq, &q) || !c.rows(K, p.Hkv, p.Nk, &k) || !c.rows(V, p.Hkv, p.Nk, &v) || !c.table(a[6], &table) ||
+      !c.lengths(a[7], &q_len) || !c.lengths(a[8], &k_len) || !O.ok([&](auto t) { return c.rows(t, p.H, p.Nq, &o); }) ||
+      !L.ok([&](auto t) { return c.flat(t, {p.B, p.H, p.Nq}, at::kFloat); }) ||
+      !ws.ok([&](auto t) { return t->device() == c.dev && bytes(t, c.fwd); }))
+    Py_RETURN_NONE;
+  if (p.Np ? !c.prefix(plain(a[4]), &kp) || !c.prefix(plain(a[5]), &vp) : a[4] != Py_None || a[5] != Py_None) Py_RETURN_NONE;
+  const bool need = a[13] == Py_True || a[11] != Py_None;
+  void* st;
+  if (!stream_of(*Q, &st)) return nullptr;
+  int rc;
+  {
+    NoGil free;
+    const c10::DeviceGuard guard(c.dev);
+    O.fill([&] { return c.fresh(*Q, p.H, p.Nq, &o); });
+    if (need) L.fill([&] { return at::empty({p.B, p.H, p.Nq}, Q->options().dtype(at::kFloat).requires_grad(false)); });
+    if (c.fwd) ws.fill([&] { return new_bytes(c.fwd, *Q); });
+    rc = sla_attn_forward(c.p, &q, &k, &v, p.Np ? &kp : nullptr, p.Np ? &vp : nullptr, table, q_len, k_len, &o,
+                          need ? (float*)L.ptr() : nullptr, c.fwd ? ws.ptr() : nullptr, c.fwd ? ws.size() : 0, st);
+  }
+  if (rc != SLA_OK) return PyLong_FromLong(rc);
+  if (!need) Py_INCREF(Py_None);
+  return pack({O.object(), need ? L.object() : Py_None});
+  END_HANDLE_TH_ERRORS
+}
+
+// attn_backward(params address, Q, K, V, O, dO, L, table, q_len, k_len, token_major, workspace, dQ, dK, dV, dtable)
+// -> (dQ, dK, dV, dtable or None)
+PyObject* attn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  AttnCall c;
+  if (n != 16) Py_RETURN_NONE;
+  const at::Tensor *Q = plain(a[1]), *K = plain(a[2]), *V = plain(a[3]), *O = plain(a[4]), *dO = plain(a[5]), *L = plain(a[6]);
+  sla_tensor q, k, v, o, go, gq, gk, gv;
+  const void* table;
+  const int32_t *q_len, *k_len;
+  Slot ws(a[11]), dQ(a[12]), dK(a[13]), dV(a[14]), dT(a[15]);
+  if (!c.open(a[0], a[10], Q)) Py_RETURN_NONE;
+  const sla_attn_params& p = *c.p;
+  if (p.Np || !c.rows(Q, p.H, p.Nq, &q) || !c.rows(K, p.Hkv, p.Nk, &k) || !c.rows(V, p.Hkv, p.Nk, &v) ||
+      !c.rows(O, p.H, p.Nq, &o) || !c.rows(dO, p.H, p.Nq, &go) || !c.flat(L, {p.B, p.H, p.Nq}, at::kFloat) ||
+      !c.table(a[7], &table) || !c.lengths(a[8], &q_len) || !c.lengths(a[9], &k_len) ||
+      !dQ.ok([&](auto t) { return c.rows(t, p.H, p.Nq, &gq); }) || !dK.ok([&](auto t) { return c.rows(t, p.Hkv, p.Nk, &gk); }) ||
+      !dV.ok([&](auto t) { return c.rows(t, p.Hkv, p.Nk, &gv); }) || (!table && a[15] != Py_None) ||
+      !dT.ok([&](auto t) { return c.flat(t, {p.buckets.n_buckets, p.H}, c.tt); }) ||
+      !ws.ok([&](auto t) { return t->device() == c.dev && bytes(t, c.bwd); }))
+    Py_RETURN_NONE;
+  void* st;
+  if (!stream_of(*Q, &st)) return nullptr;
+  int rc;
+  {
+    NoGil free;
+    const c10::DeviceGuard guard(c.dev);
+    dQ.fill([&] { return c.fresh(*Q, p.H, p.Nq, &gq); });
+    dK.fill([&] { return c.fresh(*Q, p.Hkv, p.Nk, &gk); });
+    dV.fill([&] { return c.fresh(*Q, p.Hkv, p.Nk, &gv); });
+    if (table)
+      dT.fill([&] { return at::empty({p.buckets.n_buckets, p.H}, Q->options().dtype(c.tt).requires_grad(false)); });
+    ws.fill([&] { return new_bytes(c.bwd, *Q); });
+    rc = sla_attn_backward(c.p, &q, &k, &v, &o, &go, L->const_data_ptr<float>(), table, q_len, k_len, &gq, &gk, &gv,
+                           table ? dT.ptr() : nullptr, ws.ptr(), ws.size(), st);
+  }
+  if (rc != SLA_OK) return PyLong_FromLong(rc);
+  if (!table) Py_INCREF(Py_None);
+  return pack({dQ.object(), dK.object(), dV.object(), table ? dT.object() : Py_None});
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef g_methods[] = {
     {"build_mask", (PyCFunction)(void (*)(void))build_mask, METH_FASTCALL, nullptr},
     {"forward", (PyCFunction)(void (*)(void))forward, METH_FASTCALL, nullptr},
     {"mask_forward", (PyCFunction)(void (*)(void))mask_forward, METH_FASTCALL, nullptr},
     {"backward", (PyCFunction)(void (*)(void))backward, METH_FASTCALL, nullptr},
+    {"attn_forward", (PyCFunction)(void (*)(void))attn_forward, METH_FASTCALL, nullptr},
+    {"attn_backward", (PyCFunction)(void (*)(void))attn_backward, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_sla_host", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,349 @@
+"""Softmax attention (dense_attention, cached_attention) against the formulas in 64 bits: every element within the bound
+that follows from the roundings the library makes."""
+import math
+
+import pytest
+import torch
+
+from paper_2509_24006_amd import autograd as attn
+from paper_2509_24006_amd import binding as sla
+from tests import attention_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def within(got, want, what):
+    """got [..] against (value, bound), every element"""
+    value, bound = want
+    got = got.double()
+    same = (got == value) | ((got - value).abs() <= bound + 1e-30)   # (both infinite: equal)
+    if not bool(same.all()):
+        worst = torch.where(same, torch.zeros_like(value), (got - value).abs() / (bound + 1e-30)).nan_to_num(float("inf"))
+        i = int(worst.argmax())
+        at = [int(x) for x in torch.unravel_index(torch.tensor(i), value.shape)]
+        raise AssertionError(f"{what}: {int((~same).sum())} of {same.numel()} elements out of bounds, the worst at {at}: "
+                             f"{got.flatten()[i]:.6g} for {value.flatten()[i]:.6g} +- {bound.flatten()[i]:.3g}")
+
+
+def tensors(dt, B, H, Hkv, Nq, Nk, d, seed=0, size=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda *s: (size * torch.randn(*s, generator=g, device="cuda")).to(dt)
+    return r(B, H, Nq, d), r(B, Hkv, Nk, d), r(B, Hkv, Nk, d), r(B, H, Nq, d)
+
+
+def ints(x):
+    return None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def check(dt, B, H, Hkv, Nq, Nk, d, causal=False, q_len=None, k_len=None, bias=None, table_dtype=F32, token=False, seed=0,
+          size=1.0, scale=None, garbage=False):
+    """forward and backward through autograd, and L through the binding"""
+    Q, K, V, dO = tensors(dt, B, H, Hkv, Nq, Nk, d, seed, size)
+    if garbage:   # nothing behind a length is read
+        bad = torch.tensor([math.nan, math.inf, -math.inf, torch.finfo(dt).min], device="cuda").to(dt)
+        for b in range(B):
+            for t, n in ((Q, q_len), (dO, q_len), (K, k_len), (V, k_len)):
+                if n is not None:
+                    t[b, :, max(0, n[b]):] = bad[b % 4]
+    buckets = table = None
+    if bias:
+        nb, far, two = bias
+        buckets = sla.position_buckets(nb, far, two)
+        table = torch.randn(nb, H, device="cuda", generator=torch.Generator("cuda").manual_seed(seed + 1)).to(table_dtype)
+    s = d ** -0.5 if scale is None else scale
+    want = ref.attention(Q, K, V, s, causal, q_len, k_len, [Nk - Nq] * B, table,
+                         [] if not bias else list(buckets.borders)[:nb // (2 if two else 1) - 1], bool(bias) and two,
+                         dO=dO, result=dt)
+    turn = (lambda t: t.transpose(1, 2).contiguous()) if token else (lambda t: t.clone())
+    leaves = [turn(t).requires_grad_(True) for t in (Q, K, V)]
+    tl = None if table is None else table.clone().requires_grad_(True)
+    O = attn.dense_attention(*leaves, causal=causal, scale=scale, q_len=ints(q_len), k_len=ints(k_len), table=tl,
+                             buckets=buckets, token_major=token)
+    grads = torch.autograd.grad(O, leaves + ([tl] if bias else []), turn(dO))
+    back = (lambda t: t.transpose(1, 2)) if token else (lambda t: t)
+    within(back(O), want["O"], "O")
+    for name, got in zip(("dQ", "dK", "dV"), grads):
+        within(back(got), want[name], name)
+    if bias:
+        assert grads[3].dtype == table_dtype
+        within(grads[3], want["dtable"], "dtable")
+    p = sla.make_attn_params(B, H, Hkv, Nq, Nk, d, dt, causal, scale, q_pos=Nk - Nq, buckets=buckets,
+                             table_dtype=F32 if table is None else table.dtype)
+    O2, L = sla.sla_attn_forward(p, *[t.detach() for t in leaves], table, ints(q_len), ints(k_len), token_major=token)
+    within(L, want["L"], "L")
+    assert torch.equal(O2, O.detach())
+    with torch.no_grad():   # without statistics
+        O3 = attn.dense_attention(*leaves, causal=causal, scale=scale, q_len=ints(q_len), k_len=ints(k_len), table=tl,
+                                  buckets=buckets, token_major=token)
+    assert torch.equal(O3, O.detach())
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq,Nk", [(1, 1), (1, 64), (2, 3), (17, 65), (63, 64), (64, 63), (65, 1), (128, 129), (200, 31),
+                                   (300, 257)])
+def test_rectangles(dt, d, Nq, Nk):
+    check(dt, 2, 3, 3, Nq, Nk, d)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,d", [(1, 4, 2, 1, 1, 64), (2, 4, 1, 65, 65, 64), (1, 6, 2, 130, 130, 128),
+                                             (1, 8, 8, 257, 257, 64), (2, 8, 2, 33, 200, 128), (1, 3, 1, 200, 70, 64),
+                                             (1, 2, 2, 640, 640, 128)])
+def test_causal_and_shared_heads(dt, B, H, Hkv, Nq, Nk, d):
+    # (more queries than keys: the first rows see no key at all)
+    check(dt, B, H, Hkv, Nq, Nk, d, causal=True)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("token", [False, True], ids=["head_major", "token_major"])
+@pytest.mark.parametrize("Nq,Nk,q_len,k_len", [
+    (130, 130, [130, 64, 1, 0], [130, 64, 1, 0]), (70, 200, None, [200, 129, 65, 0]), (100, 100, [100, 0, 3, 77], [0, 100, 64, 1]),
+    (64, 64, [-3, 99, 64, 5], [1 << 30, 64, -1, 65])])
+def test_lengths_and_what_lies_behind_them(dt, causal, token, Nq, Nk, q_len, k_len):
+    check(dt, 4, 4, 2, Nq, Nk, 64, causal, q_len, k_len, token=token, garbage=True)
+
+
+@pytest.mark.parametrize("dt,table_dtype", [(F32, F32), (BF, BF), (BF, F32)], ids=["fp32", "bf16", "bf16_float_table"])
+@pytest.mark.parametrize("bias", [(32, 128, True), (16, 64, False), (4, 3, True), (2, 1024, False), (64, 700, False)])
+@pytest.mark.parametrize("B,H,Hkv,N,d,causal", [(2, 3, 3, 65, 64, False), (1, 4, 2, 500, 64, True), (3, 2, 1, 200, 128, False),
+                                                (1, 1, 1, 1, 64, True)])
+def test_position_bias(dt, table_dtype, bias, B, H, Hkv, N, d, causal):
+    lens = [N - 37 * b for b in range(B)]
+    check(dt, B, H, Hkv, N, N, d, causal, lens if B > 1 else None, lens if B > 1 else None, bias, table_dtype, garbage=True)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+def test_bias_of_a_rectangle(dt):
+    check(dt, 2, 2, 2, 40, 333, 64, bias=(32, 128, True))
+    check(dt, 2, 2, 2, 333, 40, 64, causal=True, bias=(8, 20, False))
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("size,scale", [(0.01, None), (4.0, None), (1.0, 0.01), (1.0, 1.0), (30.0, 1e-4)])
+def test_score_sizes(dt, size, scale):
+    check(dt, 1, 2, 1, 150, 170, 64, size=size, scale=scale)
+
+
+def test_one_key_takes_everything():
+    # scores so far apart that one probability is 1 and the others vanish: later tiles move the maximum far
+    Q = torch.zeros(1, 1, 64, 64, device="cuda", dtype=BF)
+    K = torch.zeros(1, 1, 256, 64, device="cuda", dtype=BF)
+    Q[..., 0] = 64.0
+    K[0, 0, :, 0] = torch.arange(256, device="cuda") / 2.0
+    V = torch.randn(1, 1, 256, 64, device="cuda").to(BF)
+    O = attn.dense_attention(Q, K, V)
+    want = ref.attention(Q, K, V, 0.125, pos=[0])
+    within(O, want["O"], "O")
+
+
+# ---------------------------------------------------------------- serving
+
+def serve(dt, B, H, Hkv, Nq, Nk, d, k_len=None, Np=0, bias=None, token=False, causal=True, seed=0, garbage=True):
+    Q, K, V, _ = tensors(dt, B, H, Hkv, Nq, Nk, d, seed)
+    g = torch.Generator(device="cuda").manual_seed(seed + 5)
+    prefix = tuple(torch.randn(Hkv, Np, d, generator=g, device="cuda").to(dt) for _ in range(2)) if Np else None
+    if garbage and k_len is not None:
+        for b in range(B):
+            K[b, :, max(0, k_len[b]):] = math.nan
+            V[b, :, max(0, k_len[b]):] = math.inf
+    buckets = table = None
+    if bias:
+        buckets = sla.position_buckets(*bias)
+        table = torch.randn(bias[0], H, device="cuda", generator=g).to(dt)
+    lens = [Nk] * B if k_len is None else [min(max(x, 0), Nk) for x in k_len]
+    want = ref.attention(Q, K, V, d ** -0.5, causal, None, k_len, [Np + n - Nq for n in lens], table,
+                         [] if not bias else list(buckets.borders)[:bias[0] // (2 if bias[2] else 1) - 1],
+                         bool(bias) and bias[2], prefix, result=dt)
+    turn = (lambda t: t.transpose(-3, -2).contiguous()) if token else (lambda t: t)
+    O = attn.cached_attention(turn(Q), turn(K), turn(V), ints(k_len), None if not Np else tuple(turn(t) for t in prefix),
+                              causal, table=table, buckets=buckets, token_major=token)
+    within(O.transpose(1, 2) if token else O, want["O"], "O")
+    assert not O.requires_grad
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("token", [False, True], ids=["head_major", "token_major"])
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,d,k_len", [
+    (1, 2, 2, 1, 1, 64, None), (1, 12, 12, 1, 1000, 128, None), (5, 8, 2, 1, 700, 128, [700, 1, 0, 333, 64]),
+    (3, 4, 1, 5, 300, 64, [300, 5, 2]), (2, 6, 2, 70, 500, 64, [500, 70]), (4, 16, 1, 8, 2000, 128, [2000, 9, 8, 1500])])
+def test_new_tokens_over_a_cache(dt, token, B, H, Hkv, Nq, Nk, d, k_len):
+    serve(dt, B, H, Hkv, Nq, Nk, d, k_len, token=token)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("token", [False, True], ids=["head_major", "token_major"])
+@pytest.mark.parametrize("B,H,Hkv,Nq,Nk,d,k_len,Np", [
+    (1, 1, 1, 1, 1, 64, None, 1), (3, 4, 2, 1, 100, 128, [100, 1, 0], 500), (7, 6, 3, 3, 40, 64, [40, 3, 0, 2, 17, 39, 5], 333),
+    (2, 2, 2, 65, 65, 64, None, 130), (40, 4, 1, 1, 9, 64, None, 1111), (2, 2, 1, 2, 0, 64, None, 65)])
+def test_shared_prefix(dt, token, B, H, Hkv, Nq, Nk, d, k_len, Np):
+    serve(dt, B, H, Hkv, Nq, Nk, d, k_len, Np, token=token)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("bias", [(32, 128, False), (16, 900, True)])
+def test_bias_over_a_cache(dt, bias):
+    serve(dt, 3, 6, 2, 4, 400, 64, [400, 4, 111], 0, bias)
+    serve(dt, 3, 6, 3, 4, 100, 64, [100, 4, 11], 777, bias)
+    serve(dt, 2, 3, 3, 1, 100, 128, None, 200, bias, causal=False)
+
+
+def test_prefix_equals_the_same_rows_in_every_cache():
+    Q, K, V, _ = tensors(BF, 6, 8, 2, 2, 300, 128)
+    K[:, :, :200], V[:, :, :200] = K[:1, :, :200], V[:1, :, :200]
+    whole = attn.cached_attention(Q, K, V)
+    split = attn.cached_attention(Q, K[:, :, 200:], V[:, :, 200:], prefix=(K[0, :, :200], V[0, :, :200]))
+    want = ref.attention(Q, K, V, 128 ** -0.5, True, pos=[298] * 6)
+    within(whole, want["O"], "whole")
+    within(split, want["O"], "split")
+
+
+# ---------------------------------------------------------------- strides, streams, graphs
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+def test_slices_of_a_fused_projection_and_broadcast_heads(dt):
+    qkv = torch.randn(2, 100, 3, 4, 64, device="cuda").to(dt)
+    Q, K, V = (qkv[:, :, i] for i in range(3))
+    a = attn.dense_attention(Q, K, V, token_major=True)
+    b = attn.dense_attention(*(t.contiguous() for t in (Q, K, V)), token_major=True)
+    assert torch.equal(a, b) and a.is_contiguous()
+    # one K, V for all sequences and heads: its gradient is the sum over them
+    k = torch.randn(1, 1, 77, 64, device="cuda").to(dt).requires_grad_(True)
+    q = torch.randn(3, 2, 50, 64, device="cuda").to(dt)
+    dO = torch.randn_like(q)
+    full = k.expand(3, 2, 77, 64)
+    O = attn.dense_attention(q, full, full)
+    g, = torch.autograd.grad(O, k, dO)
+    want = ref.attention(q, full, full, 0.125, pos=[27] * 3, dO=dO, result=dt)
+    both = want["dK"][0] + want["dV"][0]
+    # (autograd adds dK and dV, then the six heads, rounding each time)
+    mag = (want["dK"][0].abs() + want["dV"][0].abs()).sum((0, 1), keepdim=True)
+    bound = (want["dK"][1] + want["dV"][1]).sum((0, 1), keepdim=True) + 3 * ref.U[dt] * mag
+    within(g, (both.sum((0, 1), keepdim=True), bound), "shared K, V")
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+def test_odd_strides_are_laid_out(dt):
+    wide = torch.randn(2, 2, 90, 67, device="cuda").to(dt)
+    Q = wide[..., 1:65]                                     # rows 67 apart, misaligned
+    K = torch.randn(2, 2, 64, 90, device="cuda").to(dt).transpose(2, 3)   # features not contiguous
+    V = torch.randn(1, 2, 1, 64, device="cuda").to(dt).expand(2, 2, 90, 64)   # rows on top of each other
+    O = attn.dense_attention(Q, K, V)
+    assert torch.equal(O, attn.dense_attention(Q.contiguous(), K.contiguous(), V.contiguous()))
+    Qg = Q.detach().contiguous().requires_grad_(True)
+    attn.dense_attention(Qg, K, V).sum().backward()         # an expanded gradient
+    assert bool(torch.isfinite(Qg.grad).all())
+
+
+def test_results_repeat_bit_for_bit():
+    for dt in (F32, BF):
+        Q, K, V, dO = tensors(dt, 2, 4, 2, 333, 333, 64)
+        table = torch.randn(32, 4, device="cuda")
+        bk = sla.position_buckets(32, 128)
+        lens = ints([333, 200])
+        runs = []
+        for _ in range(2):
+            ls = [t.clone().requires_grad_(True) for t in (Q, K, V, table)]
+            O = attn.dense_attention(*ls[:3], q_len=lens, k_len=lens, table=ls[3], buckets=bk)
+            runs.append((O.detach(),) + torch.autograd.grad(O, ls, dO))
+        assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("which", ["train", "serve"])
+def test_captured_calls_replay(which):
+    dt = BF
+    Q, K, V, dO = tensors(dt, 3, 4, 2, 90 if which == "train" else 2, 400, 64)
+    lens = ints([400, 300, 5])
+    table, bk = torch.randn(32, 4, device="cuda"), sla.position_buckets(32, 128)
+    prefix = tuple(torch.randn(2, 130, 64, device="cuda").to(dt) for _ in range(2))
+    p = sla.make_attn_params(3, 4, 2, 90, 400, 64, dt, q_pos=310, buckets=bk)
+
+    def call():
+        if which == "serve":
+            return (attn.cached_attention(Q, K, V, lens, prefix, table=table, buckets=bk),)
+        O, L = sla.sla_attn_forward(p, Q, K, V, table, None, lens)
+        return (O,) + sla.sla_attn_backward(p, Q, K, V, O, dO, L, table, None, lens)
+
+    call()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        eager_side = call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(100 + seed)
+        for t in (Q, K, V, dO):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        lens.copy_(ints([400 - 50 * seed, 300, 5 + seed]))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        want = call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
+    assert len(eager_side) == len(held)
+
+
+def test_tensor_subclasses_go_through_the_checked_calls():
+    class Mine(torch.Tensor):
+        pass
+
+    Q, K, V, dO = tensors(BF, 2, 4, 2, 70, 90, 64)
+    lens = ints([90, 33])
+    table, bk = torch.randn(8, 4, device="cuda"), sla.position_buckets(8, 20)
+    p = sla.make_attn_params(2, 4, 2, 70, 90, 64, BF, True, q_pos=20, buckets=bk)
+    O, L = sla.sla_attn_forward(p, Q, K, V, table, None, lens)
+    g = sla.sla_attn_backward(p, Q, K, V, O, dO, L, table, None, lens)
+    m = lambda t: t.as_subclass(Mine)
+    O2, L2 = sla.sla_attn_forward(p, m(Q), m(K), m(V), m(table), None, m(lens))
+    assert torch.equal(O, O2) and torch.equal(L, L2)
+    g2 = sla.sla_attn_backward(p, m(Q), K, V, O, m(dO), L, table, None, lens)
+    assert all(torch.equal(a, b) for a, b in zip(g, g2))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_gradients_against_differences(causal):
+    """central differences of the float forward pass along a direction: their error is the third
+    derivative's h^2 / 6 (scores move by at most 0.02) and float noise over h"""
+    Q, K, V, dO = tensors(F32, 1, 2, 1, 30, 41, 64, seed=3)
+    table, bk = torch.randn(8, 2, device="cuda"), sla.position_buckets(8, 20)
+    leaves = [t.clone().requires_grad_(True) for t in (Q, K, V, table)]
+    f = lambda ts: attn.dense_attention(*ts[:3], causal=causal, table=ts[3], buckets=bk)
+    grads = torch.autograd.grad(f(leaves), leaves, dO)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for i, t in enumerate(leaves):
+        step = torch.randn(t.shape, generator=g, device="cuda")
+        h = 2.0 ** -7
+        with torch.no_grad():
+            up, down = list(leaves), list(leaves)
+            up[i], down[i] = t + h * step, t - h * step
+            diff = ((f(up).double() - f(down).double()) * dO.double()).sum() / (2 * h)
+        want = (grads[i].double() * step.double()).sum()
+        size = (grads[i].double() ** 2).sum().sqrt() * (step.double() ** 2).sum().sqrt()
+        assert abs(float(diff - want)) <= 2e-3 * float(size), (i, float(diff), float(want))
+
+
+def test_layers_of_a_block_together():
+    """A block as its users build it: an SLA layer, then cross attention to a ragged text whose encoder has a position
+    bias, a dense layer on the slices of a fused projection; gradients reach every leaf."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF).requires_grad_(True)
+    B, H, N, T, d = 2, 2, 320, 50, 64
+    x, text, W, table = r(B, H, N, d), r(B, H, T, d), r(d, d), torch.randn(16, H, generator=g, device="cuda").requires_grad_(True)
+    lens = ints([50, 13])
+    bk = attn.position_buckets(16, 32)
+    enc = attn.dense_attention(text, text, text, q_len=lens, k_len=lens, table=table, buckets=bk)
+    y = attn.sla_attention(x, x, x, W, k_h=0.4, k_l=0.2)
+    z = attn.dense_attention(y, enc, enc, k_len=lens)
+    out = attn.dense_attention(z, z, z)
+    grads = torch.autograd.grad(out, (x, text, W, table), torch.ones_like(out))
+    for t, gr in zip((x, text, W, table), grads):
+        assert gr.shape == t.shape and bool(torch.isfinite(gr).all()) and float(gr.abs().max()) > 0
+    assert float(grads[1][1, :, 13:].abs().max()) == 0   # what lies behind a text's length has no part in it
