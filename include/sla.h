@@ -228,7 +228,9 @@ int sla_attn_sizes(const sla_attn_params* p, uint64_t* forward_bytes, uint64_t* 
 
 /* Kp, Vp: the prefix, or NULL where Np = 0.  table: table_dtype [n_buckets, H], or NULL without buckets.  q_len, k_len:
  * int32 [B] or NULL (all Nq, all Nk); values outside the tensor are cut to it.  O (out); L: float [B, H, Nq] (out),
- * or NULL.  workspace: >= forward_bytes (may be NULL when that is 0). */
+ * or NULL.  workspace: >= forward_bytes (may be NULL when that is 0).  SLA_EUNSUPPORTED where the keys that one
+ * workgroup reads of a head (all of them with many queries, a part with few), or with few queries (below 64) or a prefix the
+ * rows of Q or O of a sequence (behind a prefix: of the batch), span 2^31 bytes. */
 int sla_attn_forward(const sla_attn_params* p, const sla_tensor* Q, const sla_tensor* K, const sla_tensor* V,
                      const sla_tensor* Kp, const sla_tensor* Vp, const void* table, const int32_t* q_len,
                      const int32_t* k_len, const sla_tensor* O, float* L, void* workspace, size_t workspace_bytes,

@@ -110,6 +110,7 @@ int sla_attn_forward(const sla_attn_params* p, const sla_tensor* Q, const sla_te
   if (rc != SLA_OK) return rc;
   if (off(L, 4) || off(workspace, 16)) return SLA_EINVAL;
   a.L = L;
+  if (!attn_forward_fits(a)) return SLA_EUNSUPPORTED;
   const size_t need = attn_forward_ws(a);
   if (need && !workspace) return SLA_EINVAL;
   if (workspace_bytes < need) return SLA_ENOSPACE;

@@ -1,0 +1,157 @@
+// Plan of a forward pass, and the kernel that joins the sums of keys that were cut.
+#include "attn_plan.h"
+
+#include <algorithm>
+
+#include "mfma_common.h"
+
+namespace sla {
+
+namespace {
+
+constexpr int kSlots = 512;   // workgroups that run at a time: two per CU
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+AttnPart part_of(int units, int heads, long long rows, bool packed) {
+  AttnPart p = {};
+  p.units = units;
+  p.heads = heads;
+  p.rows = (int)rows;
+  p.tiles = (int)ceil_div(rows, kBlk);
+  p.splits = 1;
+  p.packed = packed;
+  return p;
+}
+
+}  // namespace
+
+AttnPlan attn_plan(const Attn& a, char* ws) {
+  AttnPlan p = {};
+  // The heads of a group share a row tile where one head's queries would leave most of it empty.  (Their bias takes
+  // LDS per head: as many as leave room for two workgroups on a CU, else one.)
+  const long long bias = a.has_bias() ? a.G * (2ll * a.bias.far + 1) * 4 : 0;
+  const bool packed = (a.Nq < kBlk || a.Np > 0) && bias <= 12 * 1024;
+  const int heads = packed ? a.G : 1;
+  p.own = part_of(a.B * a.H / heads, heads, (long long)heads * a.Nq, packed);
+  const long long T = ceil_div(a.Nk, kBlk), Tp = ceil_div(a.Np, kBlk);
+  if (a.Np > 0) p.prefix = part_of(a.H / heads, heads, (long long)a.B * heads * a.Nq, true);
+  // Parts of about equal length that fill the chip once, two key tiles or more each (less does not pay for a part's
+  // fixed cost and its sums).
+  const long long tiles = (long long)p.own.units * p.own.tiles, ptiles = (long long)p.prefix.units * p.prefix.tiles;
+  const long long len = std::max(2ll, ceil_div(tiles * T + ptiles * Tp, kSlots));
+  p.own.splits = (int)std::max(1ll, std::min(ceil_div(T, len), 256ll));
+  p.prefix.splits = (int)std::max(1ll, std::min(ceil_div(Tp, len), 256ll));
+  p.parts = a.Np > 0 || p.own.splits > 1;
+  if (p.parts) {
+    p.own.blocks = (int)(tiles * p.own.splits);
+    p.prefix.blocks = (int)(ptiles * p.prefix.splits);
+    p.own.slot0 = p.prefix.blocks;
+    p.slots = p.own.slot0 + p.own.blocks;
+    p.part = reinterpret_cast<float*>(ws);
+    p.stat = reinterpret_cast<float*>(ws + align_up((size_t)p.slots * kBlk * a.d * 4));
+  }
+  return p;
+}
+
+size_t attn_plan_ws(const Attn& a, const AttnPlan& p) {
+  return p.parts ? align_up((size_t)p.slots * kBlk * a.d * 4) + align_up((size_t)p.slots * kBlk * 8) : 0;
+}
+
+bool attn_forward_fits(const Attn& a) {
+  const AttnPlan p = attn_plan(a, nullptr);
+  constexpr long long lim = (1ll << 31) - (1 << 17);
+  const long long esz = a.dtype == SLA_F32 ? 4 : 2;
+  // keys of one workgroup behind one descriptor
+  auto span = [&](const View& v, long long tiles, int splits) { return (ceil_div(tiles, splits) + 1) * kBlk * v.sn * esz; };
+  const long long T = ceil_div(a.Nk, kBlk), Tp = ceil_div(a.Np, kBlk);
+  if (span(a.K, T, p.own.splits) >= lim || span(a.V, T, p.own.splits) >= lim) return false;
+  if (a.Np && (span(a.Kp, Tp, p.prefix.splits) >= lim || span(a.Vp, Tp, p.prefix.splits) >= lim)) return false;
+  // rows of a packed unit (those of one head are counted from their tile)
+  if (p.own.packed || a.Np) {
+    auto rows = [&](const View& v) { return ((a.Np ? a.B - 1 : 0) * v.sb + (p.own.heads - 1) * v.sh + (long long)(a.Nq - 1) * v.sn + a.d) * esz; };
+    if (rows(a.Q) >= lim || rows(a.O) >= lim) return false;
+  }
+  return true;
+}
+
+namespace {
+
+__device__ __forceinline__ void put_pair(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = float2{x, y}; }
+__device__ __forceinline__ void put_pair(bf16* p, float x, float y) {
+  bf16x2 v;
+  v[0] = (__bf16)x;
+  v[1] = (__bf16)y;
+  *reinterpret_cast<bf16x2*>(p) = v;
+}
+__device__ __forceinline__ void put_one(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put_one(bf16* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }
+
+// O = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i over the parts of a row, a wave per row.  The order is that of the parts.
+template <class E, int D>
+__global__ __launch_bounds__(256) void attn_join_kernel(Attn a, AttnPlan plan) {
+  const int l = threadIdx.x & 63;
+  const long long row = (long long)blockIdx.x * 4 + wave_uniform(threadIdx.x >> 6);
+  if (row >= (long long)a.B * a.H * a.Nq) return;
+  const int n = row % a.Nq, bh = row / a.Nq, b = bh / a.H, h = bh - b * a.H;
+  const AttnPart &ow = plan.own, &pp = plan.prefix;
+  const int u = h / ow.heads, hg = h - u * ow.heads;
+  // first slot and row of this query among the prefix's and its own sums
+  const int pr = (b * ow.heads + hg) * a.Nq + n, orow = ow.packed ? hg * a.Nq + n : n;
+  const size_t ps = pp.blocks ? ((size_t)u * pp.tiles + pr / kBlk) * pp.splits : 0;
+  const size_t os = ow.slot0 + ((size_t)(b * (a.H / ow.heads) + u) * ow.tiles + orow / kBlk) * ow.splits;
+  const int np = pp.blocks ? pp.splits : 0, total = np + ow.splits;
+  auto at = [&](int i) { return i < np ? (ps + i) * kBlk + pr % kBlk : (os + i - np) * kBlk + orow % kBlk; };
+  // statistics: part i in lane i, i + 64, ...
+  float M = -INFINITY;
+  for (int i = l; i < total; i += 64) {
+    const float2 x = *reinterpret_cast<const float2*>(plan.stat + 2 * at(i));
+    if (x.y > 0.0f) M = fmaxf(M, x.x);
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+  float lsum = 0.0f, acc[D / 64] = {};
+  for (int i0 = 0; i0 < total; i0 += 64) {
+    float2 x = {0.0f, 0.0f};
+    if (i0 + l < total) x = *reinterpret_cast<const float2*>(plan.stat + 2 * at(i0 + l));
+    const float wt = x.y > 0.0f ? fast_exp2(x.x - M) : 0.0f;
+    float s = wt * x.y;
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+    lsum += s;
+    const int cnt = min(64, total - i0);
+#pragma unroll 4
+    for (int i = 0; i < cnt; ++i) {
+      const float wi = __shfl(wt, i);
+      if (wi == 0.0f) continue;   // (sums of a part without a key are not written)
+      const float* p = plan.part + at(i0 + i) * D + (D / 64) * l;
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(wi, p[e], acc[e]);
+    }
+  }
+  const float inv = lsum > 0.0f ? 1.0f / lsum : 0.0f;
+  E* o = reinterpret_cast<E*>(a.O.p) + b * a.O.sb + h * a.O.sh + (long long)n * a.O.sn + (D / 64) * l;
+  if constexpr (D == 128) put_pair(o, acc[0] * inv, acc[1] * inv);
+  else put_one(o, acc[0] * inv);
+  if (a.L && l == 0) a.L[row] = lsum > 0.0f ? M * kLn2 + logf(lsum) : -INFINITY;
+}
+
+}  // namespace
+
+hipError_t attn_join(const Attn& a, const AttnPlan& plan, hipStream_t st) {
+  const unsigned grid = (unsigned)(((long long)a.B * a.H * a.Nq + 3) / 4);
+  auto kern = a.dtype == SLA_F32 ? (a.d == 64 ? attn_join_kernel<float, 64> : attn_join_kernel<float, 128>)
+                                 : (a.d == 64 ? attn_join_kernel<bf16, 64> : attn_join_kernel<bf16, 128>);
+  KernelTimer kt("attn_join", st);
+  kern<<<grid, 256, 0, st>>>(a, plan);
+  return hipGetLastError();
+}
+
+size_t attn_forward_ws(const Attn& a) { return a.dtype == SLA_F32 ? 0 : attn_plan_ws(a, attn_plan(a, nullptr)); }
+
+hipError_t attn_forward(const Attn& a, char* ws, hipStream_t st) {
+  if (a.dtype == SLA_F32) return attn_forward_f32(a, st);
+  return attn_forward_bf16(a, attn_plan(a, ws), st);
+}
+
+}  // namespace sla
