@@ -1,0 +1,733 @@
+// bf16 softmax attention, backward pass on the matrix cores.  The probabilities are formed again from the scores and L.
+//   attn_dq_kernel   one workgroup per 64 queries of a head: D = rowsum(dO O), dQ, and its part of the bias table's gradient
+//   attn_dkdv_kernel one workgroup per 64 keys (and piece of the queries): dK, dV summed over the queries of all heads
+//                    that read them; its last workgroups add up the table's gradient
+//   attn_kv_join     adds the pieces
+// S and dP are formed in both kernels (seven products instead of five): dQ summed where dK and dV are would need float
+// atomics of a 64 x d tile per pair, whose order changes the result and whose traffic costs more than the two products.
+// P and dS enter their second products rounded to bf16, the matrix cores' operand type; all sums are in float.
+#include <math.h>
+
+#include "attn.h"
+#include "mfma_common.h"
+
+namespace sla {
+namespace {
+
+template <int D>
+__device__ __forceinline__ BufDesc rows_rsrc(const View& v, int b, int h, int n) {
+  const bf16* p = reinterpret_cast<const bf16*>(v.p) + (size_t)b * v.sb + (size_t)h * v.sh;
+  return tile_rsrc(p, (max(n, 1) - 1) * 2 * v.sn + 2 * D);
+}
+
+// bias in log2 units by distance, 2 far + 1 floats
+__device__ __forceinline__ void expand_bias(const Attn& a, int h, float* out) {
+  for (int i = threadIdx.x; i <= 2 * a.bias.far; i += 256) out[i] = table_at(a, bucket_of(a.bias, i - a.bias.far), h) * kLog2e;
+}
+
+// ------------------------------------------------------------------ dQ
+template <int D>
+struct DqLds {
+  static constexpr int TILE = SwzTile<D>::BYTES;
+  static constexpr int BUF = 2 * TILE;             // K_j and V_j
+  static constexpr int SP = D + 4;                 // floats per row of the output staging
+  static constexpr int FIXED = 2 * BUF > kBlk * SP * 4 ? 2 * BUF : kBlk * SP * 4;
+  // with a bias: the bias by distance, then the sums of dS by distance, one array per wave and lane half
+  static constexpr int BIAS = FIXED;
+};
+__host__ __device__ inline int dq_bias_lds(int far) { return 9 * (2 * far + 1) * 4 + 32; }
+
+// Wave (qh, kh): S^T and dP^T are [key][query], one query per lane, so L and D are per-lane scalars and dS^T feeds
+// dQ^T = K^T dS^T from registers.  The two kh waves hold sums over their keys and are added at the end.
+//
+// The table's gradient is a sum of dS by distance.  Away from the diagonal a lane's values all belong to the last bucket
+// of a side, and stay in a register; near it a value is added in LDS at its distance.  The 32 lanes of a half hold
+// consecutive queries, so the distances of one instruction differ, and every half of every wave has an array of its own:
+// the order of the additions is fixed.
+template <int D, bool BIAS>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, AttnGrads gr, float* __restrict__ Ds,
+                                                                        float* __restrict__ tpart, int tiles) {
+  using Lds = DqLds<D>;
+  using T = SwzTile<D>;
+  constexpr int NT = D / 32, KT = D / 16, RB = 16 * T::ROW_BYTES;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 5, ln = l & 31;
+  const int qh = w & 1, kh = w >> 1;
+  const BlockOf own = block_of(blockIdx.y, blockIdx.x, a.B * a.H, tiles);
+  if (own.i < 0) return;
+  const int bh = wave_uniform(own.bh), i = wave_uniform(a.causal ? tiles - 1 - own.i : own.i);   // (longest rows first)
+  const int b = bh / a.H, h = bh - b * a.H, hk = h / a.G;
+  const Seq s = seq_of(a, b);
+  const int q0 = i * kBlk, rows = min(kBlk, a.Nq - q0), n = q0 + qh * 32 + ln;
+  const bool live = n < s.nq;
+  const int pos = s.pos + n;
+  int limmax = q0 < s.nq ? s.nk : 0;
+  if (a.causal) limmax = max(0, min(limmax, s.pos + min(q0 + kBlk, s.nq)));
+  const int steps = wave_uniform((limmax + kBlk - 1) / kBlk);
+  const int lim = !live ? 0x7fffffff : a.causal ? max(0, min(s.nk, pos + 1)) : s.nk;   // (rows that are not live: dO = 0)
+  const float sl2 = a.scale * kLog2e;
+
+  TileLoader<D> tq, tg, tk, tv;
+  tq.init(lds_base(smem), w, l, 2 * a.Q.sn);
+  tg.init(lds_base(smem), w, l, 2 * gr.dO.sn);
+  tk.init(lds_base(smem), w, l, 2 * a.K.sn);
+  tv.init(lds_base(smem), w, l, 2 * a.V.sn);
+  tq.load(rows_rsrc<D>(a.Q, b, h, s.nq), i, Lds::BUF);
+  tg.load(rows_rsrc<D>(gr.dO, b, h, s.nq), i, Lds::BUF + Lds::TILE);
+  const size_t li = (size_t)bh * a.Nq + n;
+  float Lq = live ? a.L[li] * kLog2e : INFINITY;
+  if (Lq == -INFINITY) Lq = INFINITY;   // (a row without a key: P = 0)
+  bf16x8 of[KT];
+  {
+    const bf16* o = reinterpret_cast<const bf16*>(a.O.p) + (size_t)b * a.O.sb + (size_t)h * a.O.sh + (size_t)min(n, a.Nq - 1) * a.O.sn;
+#pragma unroll
+    for (int t = 0; t < KT; ++t) of[t] = *reinterpret_cast<const bf16x8*>(o + 16 * t + 8 * g);
+  }
+  float* const bias = reinterpret_cast<float*>(smem + Lds::BIAS);
+  const int far = a.bias.far, width = 2 * far + 1;
+  float* const dist = bias + width;                    // [wave][half][width]
+  float* const mine = dist + (2 * w + g) * width;
+  if constexpr (BIAS) {
+    expand_bias(a, h, bias);
+    for (int x = tid; x < 8 * width; x += 256) dist[x] = 0.0f;
+  }
+  wait_vm0_known();
+  __syncthreads();
+  bf16x8 qf[KT], gf[KT];
+  {
+    TileAddr<D> qa;
+    qa.init(32 * qh, l);
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      qf[t] = lds_row(smem, qa.row(t) + Lds::BUF);
+      gf[t] = lds_row(smem, qa.row(t) + Lds::BUF + Lds::TILE);
+    }
+  }
+  const BufDesc descK = rows_rsrc<D>(a.K, b, hk, s.nk), descV = rows_rsrc<D>(a.V, b, hk, s.nk);
+  auto issue = [&](int j, const int bufi) __attribute__((always_inline)) {
+    tk.load(descK, j, bufi * Lds::BUF);
+    tv.load(descV, j, bufi * Lds::BUF + Lds::TILE);
+  };
+  if (steps > 0) issue(0, 0);
+  float dsum = 0.0f;
+#pragma unroll
+  for (int t = 0; t < KT; ++t) {
+    pin_loaded(qf[t]);
+    pin_loaded(gf[t]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dsum = fmaf((float)gf[t][e], (float)of[t][e], dsum);
+  }
+  dsum = live ? half_sum(dsum) : 0.0f;
+  if (kh == 0 && g == 0 && live) Ds[li] = dsum;
+  const float nDq = -dsum;
+  f32x16 dqT[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) dqT[t] = zero_f32x16();
+  float sumL = 0.0f, sumR = 0.0f;   // dS at distances of -far and less, far and more
+  TileAddr<D> ad;   // this wave reads rows 32 kh .. of K_j and V_j
+  ad.init(32 * kh, l);
+  auto step = [&](int j, const int buf) __attribute__((always_inline)) {
+    const int KO = buf * Lds::BUF, VO = KO + Lds::TILE;
+    const int key0 = j * kBlk + 32 * wave_uniform(kh);
+    ad.refresh();
+    wait_vm0();
+    __syncthreads();   // tiles of step j have landed for every wave; step j - 1 is fully consumed
+    if (j + 1 < steps) issue(j + 1, buf ^ 1);
+    bf16x8 ka[KT], va[KT], ta[2][NT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      ka[t] = lds_row(smem, ad.row(t) + KO);
+      va[t] = lds_row(smem, ad.row(t) + VO);
+    }
+    sched_fence();
+    f32x16 sT = zero_f32x16(), dpT;   // (dP starts at -D of the lane's query)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dpT[r] = nDq;
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      sT = mfma32(ka[t], qf[t], sT);
+      dpT = mfma32(va[t], gf[t], dpT);
+    }
+    // K_j^T for the third product arrives under the exponentials
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int dt = 0; dt < NT; ++dt)
+        ta[u][dt] = lds_tr<D>(smem, ad.tr(0, dt) + KO + u * RB, ad.tr(1, dt) + KO + u * RB);
+    sched_fence();
+    const int d0 = key0 - pos;   // distance of this wave's first key
+    bool near = false;
+    if constexpr (BIAS) {
+      near = __any(d0 + 31 > -far && d0 < far);
+      if (near) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int x = min(max(d0 + c_row(r, g), -far), far) + far;
+          sT[r] = fast_exp2(fmaf(sT[r], sl2, bias[x] - Lq));
+        }
+      } else {
+        const float bc = bias[d0 < 0 ? 0 : 2 * far] - Lq;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sT[r] = fast_exp2(fmaf(sT[r], sl2, bc));
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sT[r] = fast_exp2(fmaf(sT[r], sl2, -Lq));
+    }
+    if (__any(lim < key0 + 32)) {
+      int first = lim - key0;
+      asm volatile("" : "+v"(first));   // (the comparisons stay inside the branch)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (c_row(r, g) >= first) sT[r] = 0.0f;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dpT[r] = sT[r] * dpT[r];
+    if constexpr (BIAS) {
+      if (near) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int x = d0 + c_row(r, g);
+          sumL += x <= -far ? dpT[r] : 0.0f;
+          sumR += x >= far ? dpT[r] : 0.0f;
+          if (x > -far && x < far) atomicAdd(mine + x + far, dpT[r]);
+        }
+      } else {
+        float x = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x += dpT[r];
+        sumL += d0 < 0 ? x : 0.0f;
+        sumR += d0 < 0 ? 0.0f : x;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8 sb = c_to_operand(dpT, u);
+#pragma unroll
+      for (int dt = 0; dt < NT; ++dt) dqT[dt] = mfma32(ta[u][dt], sb, dqT[dt]);   // K_j^T dS^T
+    }
+  };
+  for (int j = 0; j < steps; j += 2) {
+    step(j, 0);
+    if (j + 1 < steps) step(j + 1, 1);
+  }
+  // ---- add the two key halves in a row-major staging area, then every thread stores 8-byte pieces of whole rows
+  __syncthreads();   // every wave is done with the tiles
+  constexpr int C4 = D / 4, NIT = kBlk * C4 / 256, SP = Lds::SP;
+  float* stg = reinterpret_cast<float*>(smem);   // [64 queries][SP]
+  const int srow = (qh * 32 + ln) * SP + 4 * g;
+  if (kh == 1) {
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4*>(stg + srow + 32 * dt + 8 * r4) =
+            f32x4{dqT[dt][4 * r4], dqT[dt][4 * r4 + 1], dqT[dt][4 * r4 + 2], dqT[dt][4 * r4 + 3]};
+  }
+  if constexpr (BIAS) {
+    // the far sums of the four waves, and the eight arrays into the first
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+      sumL += __shfl_xor(sumL, o);
+      sumR += __shfl_xor(sumR, o);
+    }
+    if (l == 0) {
+      dist[8 * width + w] = sumL;
+      dist[8 * width + 4 + w] = sumR;
+    }
+    for (int x = tid; x < width; x += 256) {
+      float t = dist[x];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) t += dist[e * width + x];
+      dist[x] = t;
+    }
+  }
+  __syncthreads();
+  if (kh == 0) {
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        f32x4 x = *reinterpret_cast<const f32x4*>(stg + srow + 32 * dt + 8 * r4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = live ? x[r] + dqT[dt][4 * r4 + r] : 0.0f;
+        *reinterpret_cast<f32x4*>(stg + srow + 32 * dt + 8 * r4) = x;
+      }
+  }
+  if constexpr (BIAS) {
+    // bucket by bucket: the distances [n0, n1) of a side, the last bucket with the far sum
+    const int nb = bucket_count(a.bias), side = a.bias.n_borders + 1;
+    if (tid >= 256 - nb) {
+      const int u = 255 - tid, v = u >= side ? u - side : u;
+      const bool right = u >= side;
+      const int n0 = v ? a.bias.borders[v - 1] : 0, n1 = v < side - 1 ? a.bias.borders[v] : far;
+      float t = 0.0f;
+      for (int x = n0; x < n1; ++x)
+        if (!right || x > 0) t += dist[right ? far + x : far - x];
+      const float* e = dist + 8 * width + (right ? 4 : 0);
+      const float sr = (dist[8 * width + 4] + dist[8 * width + 5]) + (dist[8 * width + 6] + dist[8 * width + 7]);
+      if (v == side - 1) t += (e[0] + e[1]) + (e[2] + e[3]);
+      if (!a.bias.two_sided && v == 0) {   // keys behind the query
+        for (int x = 1; x < far; ++x) t += dist[far + x];
+        t += sr;
+      }
+      tpart[((size_t)bh * tiles + i) * nb + u] = t;
+    }
+  }
+  __syncthreads();
+  bf16* const dQ = reinterpret_cast<bf16*>(gr.dQ.p) + (size_t)b * gr.dQ.sb + (size_t)h * gr.dQ.sh + (size_t)q0 * gr.dQ.sn;
+#pragma unroll
+  for (int it = 0; it < NIT; ++it) {
+    const int idx = it * 256 + tid, row = idx / C4, c4 = idx % C4;
+    if (row < rows) {
+      const f32x4 sv = *reinterpret_cast<const f32x4*>(stg + row * SP + 4 * c4);
+      bf16x4 pk;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) pk[r] = (__bf16)(sv[r] * a.scale);
+      *reinterpret_cast<bf16x4*>(dQ + (size_t)row * gr.dQ.sn + 4 * c4) = pk;
+    }
+  }
+}
+
+// The gradient of one head's column of the table: the sum of the parts [b][tile], in an order fixed by their number.
+__device__ __forceinline__ void table_sum(const Attn& a, const AttnGrads& gr, const float* tpart, int tiles, int h,
+                                          unsigned char* smem) {
+  float* red = reinterpret_cast<float*>(smem);   // [slice][nb]
+  const int nb = bucket_count(a.bias), slices = 256 / nb, u = threadIdx.x % nb, sl = threadIdx.x / nb;
+  const int total = a.B * tiles;
+  if (sl < slices) {
+    float s = 0.0f;
+#pragma unroll 4
+    for (int x = sl; x < total; x += slices) {
+      const int b = x / tiles, t = x - b * tiles;
+      s += tpart[(((size_t)b * a.H + h) * tiles + t) * nb + u];
+    }
+    red[sl * nb + u] = s;
+  }
+  __syncthreads();
+  if ((int)threadIdx.x < nb) {
+    float s = 0.0f;
+    for (int x = 0; x < slices; ++x) s += red[x * nb + threadIdx.x];
+    const size_t at = (size_t)threadIdx.x * a.H + h;
+    if (a.table16) reinterpret_cast<__bf16*>(gr.dtable)[at] = (__bf16)s;
+    else reinterpret_cast<float*>(gr.dtable)[at] = s;
+  }
+}
+
+// ------------------------------------------------------------------ dK, dV
+// First products (S, dP): wave (kh, x) takes keys 32 kh .., queries 32 x .. of the pair; S and dP are [query][key], one
+// key per lane.  Second products (dV^T = dO^T P, dK^T = Q^T dS): the same wave takes keys 32 kh .. and the
+// feature half x, over all 64 queries.  P and dS cross between the two waves of a key half through LDS in operand layout.
+// L and D of a query enter the first products as one more k-step: the A operand carries L / scale resp. D split into three
+// bf16 terms (24 bits), the B operand -1, so that the accumulators come out as S - L / scale and dP - D.
+template <int D>
+struct DkLds {
+  static constexpr int TILE = SwzTile<D>::BYTES;
+  static constexpr int BUF = 2 * TILE;                   // Q_i and dO_i of a pair
+  static constexpr int XOFF = 2 * BUF;                   // exchange: [kh][k-step 0..3][P | dS][lane] x 16 bytes
+  static constexpr int XBYTES = 2 * 4 * 2 * 64 * 16;
+  static constexpr int BIAS = XOFF + XBYTES;
+  static constexpr int STG = 32 * (64 * (D / 64) + 16);  // output staging of one wave, laid over the tiles
+};
+
+// The steps of a key tile run over the query tiles from the first that sees it, head by head.  Above `piece` of them they
+// are cut: piece p leaves its sums in slot unit * pieces + p, and attn_kv_join adds them.
+struct KeyPlan {
+  int tiles, pieces, piece;   // key tiles; most pieces of one, steps in a piece
+  float* part;                // [B Hkv tiles][pieces] slots of 2 x 64 x d floats
+  int blocks;                 // workgroups of one piece index
+};
+struct KeySteps {
+  int i0, per_head, total;    // first query tile, tiles per head, steps
+};
+__device__ __forceinline__ KeySteps key_steps(const Attn& a, const Seq& s, int j) {
+  KeySteps k;
+  k.i0 = a.causal ? max(0, j * kBlk - s.pos) / kBlk : 0;
+  k.per_head = j * kBlk < s.nk ? max(0, (s.nq + kBlk - 1) / kBlk - k.i0) : 0;
+  k.total = k.per_head * a.G;
+  return k;
+}
+template <int D>
+__device__ __forceinline__ f32x4* key_slot(const KeyPlan& kp, size_t slot, int w, int l) {
+  return reinterpret_cast<f32x4*>(kp.part + slot * (2 * kBlk * D)) + w * (D / 8 * 64) + l;
+}
+template <int D>
+__device__ __forceinline__ void store_keys(const Attn& a, const AttnGrads& gr, unsigned char* stage, f32x16 (&dvT)[D / 64],
+                                           f32x16 (&dkT)[D / 64], int b, int hk, int j, int kh, int xh, bool ok, int l) {
+  const int rows = a.Nk - j * kBlk - 32 * kh;
+#pragma unroll
+  for (int dt = 0; dt < D / 64; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dvT[dt][r] = ok ? dvT[dt][r] : 0.0f;
+      dkT[dt][r] = ok ? dkT[dt][r] * a.scale : 0.0f;
+    }
+  auto at = [&](const View& v) {
+    return reinterpret_cast<bf16*>(v.p) + (size_t)b * v.sb + (size_t)hk * v.sh + (size_t)(j * kBlk + 32 * kh) * v.sn + (D / 2) * xh;
+  };
+  store_rows_bf16<D / 64>(stage, dvT, at(gr.dV), gr.dV.sn, rows, l);
+  store_rows_bf16<D / 64>(stage, dkT, at(gr.dK), gr.dK.sn, rows, l);
+}
+
+template <int D, bool BIAS>
+__global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(Attn a, AttnGrads gr, const float* __restrict__ Ds, KeyPlan kp,
+                                                            const float* __restrict__ tpart, int qtiles) {
+  using Lds = DkLds<D>;
+  using T = SwzTile<D>;
+  constexpr int NT = D / 32, KT = D / 16, HT = NT / 2;
+  constexpr int RB = 16 * T::ROW_BYTES;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  if ((int)blockIdx.x >= kp.blocks * kp.pieces) {
+    if constexpr (BIAS) table_sum(a, gr, tpart, qtiles, blockIdx.x - kp.blocks * kp.pieces, smem);
+    return;
+  }
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 5, ln = l & 31;
+  const int kh = w & 1, xh = w >> 1;
+  const int p = blockIdx.x / kp.blocks, bx = blockIdx.x - p * kp.blocks, brow = block_row(kp.tiles);
+  const BlockOf own = block_of(bx / brow, bx % brow, a.B * a.Hkv, kp.tiles);
+  if (own.i < 0) return;
+  const int bh = wave_uniform(own.bh), j = wave_uniform(own.i);
+  const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
+  const Seq sq = seq_of(a, b);
+  const KeySteps ks_ = key_steps(a, sq, j);
+  const int s_beg = wave_uniform(p * kp.piece), s_end = wave_uniform(min(ks_.total, s_beg + kp.piece));
+  if (p > 0 && s_beg >= s_end) return;
+  const bool cut = ks_.total > kp.piece;
+  const int cnt = s_end - s_beg;
+  const int k0 = j * kBlk, key = k0 + kh * 32 + ln;
+  const bool kok = key < sq.nk;
+  bf16x8 kf[KT], vf[KT];
+  f32x16 dvT[HT], dkT[HT];
+#pragma unroll
+  for (int t = 0; t < HT; ++t) {
+    dvT[t] = zero_f32x16();
+    dkT[t] = zero_f32x16();
+  }
+  const float sl2 = a.scale * kLog2e, rscale = 1.0f / a.scale;
+  const int wu = wave_uniform(w);
+  TileLoader<D> tq, tg;
+  tq.init(lds_base(smem), w, l, 2 * a.Q.sn);
+  tg.init(lds_base(smem), w, l, 2 * gr.dO.sn);
+  // head and query tile of the step in flight or in use (cur) and of the one after it
+  struct At {
+    int h, i;
+  };
+  const int i_end = ks_.i0 + ks_.per_head;
+  auto after = [&](At x) __attribute__((always_inline)) { return x.i + 1 < i_end ? At{x.h, x.i + 1} : At{x.h + 1, ks_.i0}; };
+  At cur{hk * a.G, ks_.i0};
+  if (cnt > 0) {
+    const int hh = s_beg / ks_.per_head;
+    cur = At{wave_uniform(hk * a.G + hh), wave_uniform(ks_.i0 + s_beg - hh * ks_.per_head)};
+  }
+  auto issue = [&](At x, const int bufi) __attribute__((always_inline)) {
+    const int off = bufi * Lds::BUF;
+    tq.load(rows_rsrc<D>(a.Q, b, x.h, sq.nq), x.i, off);
+    tg.load(rows_rsrc<D>(gr.dO, b, x.h, sq.nq), x.i, off + Lds::TILE);
+  };
+  {
+    TileLoader<D> t;
+    t.init(lds_base(smem), w, l, 2 * a.K.sn);
+    t.load(rows_rsrc<D>(a.K, b, hk, sq.nk), j, Lds::BUF);
+    t.init(lds_base(smem), w, l, 2 * a.V.sn);
+    t.load(rows_rsrc<D>(a.V, b, hk, sq.nk), j, Lds::BUF + Lds::TILE);
+  }
+  if (cnt > 0) issue(cur, 0);
+  float* const bias = reinterpret_cast<float*>(smem + Lds::BIAS);
+  const int far = a.bias.far;
+  if constexpr (BIAS) expand_bias(a, min(cur.h, a.H - 1), bias);
+  wait_vm0_known();
+  __syncthreads();
+  {
+    TileAddr<D> ka;
+    ka.init(32 * kh, l);
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      kf[t] = lds_row(smem, ka.row(t) + Lds::BUF);
+      vf[t] = lds_row(smem, ka.row(t) + Lds::BUF + Lds::TILE);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < KT; ++t) {
+    pin_loaded(kf[t]);
+    pin_loaded(vf[t]);
+  }
+  TileAddr<D> ad;   // first products: rows 32 x .. of Q_i, dO_i by rows
+  ad.init(32 * xh, l);
+  TileAddr<D> at;   // second products: transposing reads, feature tiles x HT ..
+  at.init(0, l);
+  bf16x8 bneg;      // B operand of the extra k-step: -1 at k = 0, 1, 2
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bneg[e] = (__bf16)((g == 0 && e < 3) ? -1.0f : 0.0f);
+  const int xw = Lds::XOFF + ((kh * 4 + 2 * xh) * 2 * 64 + l) * 16;   // this wave's exchange writes
+  const int xr = Lds::XOFF + (kh * 4 * 2 * 64 + l) * 16;              // ... and reads
+  const int xwave = Lds::XOFF + (kh * 4 + 2 * xh) * 2 * 64 * 16;      // start of this wave's part (uniform)
+  const unsigned xstat = lds_base(smem) + wave_uniform(xwave);
+  At next = after(cur);
+  auto step = [&](int s, const int buf) __attribute__((always_inline)) {
+    const int QO = buf * Lds::BUF, GO = QO + Lds::TILE;
+    ad.refresh();
+    at.refresh();
+    wait_vm0_known();
+    __syncthreads();   // tiles of step s have landed for every wave; step s-1 is fully consumed
+    // L and D of this step's 64 queries are requested ahead of the next pair's tiles (loads return in order) and picked
+    // up after the first products.  They go global -> LDS into the first 512 bytes of this wave's own part of the exchange
+    // area, which it overwrites with P and dS only after it has read them back.  Rows past the end read as 0; their Q
+    // and dO rows are zero too, so the finite P they get adds nothing.
+    {
+      const int n0 = cur.i * kBlk, rows = min(kBlk, sq.nq - n0), lo = lane_id() * 4;
+      const size_t li = ((size_t)b * a.H + cur.h) * a.Nq + n0;
+      load_to_lds4(tile_rsrc(a.L + li, rows * 4), lo, xstat);
+      load_to_lds4(tile_rsrc(Ds + li, rows * 4), lo, xstat + 256);
+    }
+    const int qt = cur.i;
+    // (the last step requests its own pair once more, into the other buffer, where nobody reads it: every step then
+    // has the same number of loads in flight and one wait serves all)
+    const At from = s + 1 < s_end ? next : cur;
+    issue(from, buf ^ 1);
+    cur = from;
+    next = after(from);
+    constexpr int PF = 4;   // LDS reads run PF operand pairs ahead of the products
+    bf16x8 qa[PF], ga[PF];
+    auto read_s = [&](int t) __attribute__((always_inline)) {
+      qa[t % PF] = lds_row(smem, ad.row(t) + QO);
+      ga[t % PF] = lds_row(smem, ad.row(t) + GO);
+    };
+#pragma unroll
+    for (int t = 0; t < PF; ++t) read_s(t);
+    sched_fence();
+    f32x16 sm = zero_f32x16(), dp = zero_f32x16();
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      sm = mfma32(qa[t % PF], kf[t], sm);
+      dp = mfma32(ga[t % PF], vf[t], dp);
+      if (t + PF < KT) read_s(t + PF);
+      sched_fence();
+    }
+    wait_vm<2 * T::IPW>();   // the statistics are there, the tile loads may still fly
+    {
+      const int qo = (32 * xh + (lane_id() & 31)) * 4;
+      const float lraw = *reinterpret_cast<const float*>(smem + xwave + qo);
+      const float dcur = *reinterpret_cast<const float*>(smem + xwave + 256 + qo);
+      const float lcur = lraw == -INFINITY ? 1e30f : lraw * rscale;   // (a row without a key: P = 0)
+      bf16x8 aL = zero_bf16x8(), aD = zero_bf16x8();
+      const __bf16 l0 = (__bf16)lcur, d0 = (__bf16)dcur;
+      const float lr = lcur - (float)l0, dr = dcur - (float)d0;
+      const __bf16 l1 = (__bf16)lr, d1 = (__bf16)dr;
+      const __bf16 l2 = (__bf16)(lr - (float)l1), d2 = (__bf16)(dr - (float)d1);
+      const __bf16 z = (__bf16)0.0f;
+      aL[0] = g == 0 ? l0 : z;
+      aL[1] = g == 0 ? l1 : z;
+      aL[2] = g == 0 ? l2 : z;
+      aD[0] = g == 0 ? d0 : z;
+      aD[1] = g == 0 ? d1 : z;
+      aD[2] = g == 0 ? d2 : z;
+      sm = mfma32(aL, bneg, sm);
+      dp = mfma32(aD, bneg, dp);
+    }
+    // operand i of the second products: i = 2 HT ks + 2 dt + which; which 0: dO^T rows of feature tile x HT + dt (for
+    // dV), which 1: Q^T (for dK); k = pair rows 16 ks ..
+    constexpr int PT = 6, NOP = 8 * HT;
+    bf16x8 ta[PT];
+    auto read_t = [&](int i) __attribute__((always_inline)) {
+      const int ks = i / (2 * HT), et = xh * HT + (i % (2 * HT)) / 2, base = (i % 2 ? QO : GO) + ks * RB;
+      ta[i % PT] = lds_tr<D>(smem, at.tr(0, et) + base, at.tr(1, et) + base);
+    };
+#pragma unroll
+    for (int i = 0; i < PT; ++i) read_t(i);
+    sched_fence();
+    // P = exp(S - L), dS = P (dP - D).  A lane past the end of the keys (its K and V rows are zero) computes values that
+    // stay in its own columns of dK^T and dV^T, which are written as zeros.
+    const int e0 = key - sq.pos - qt * kBlk - 32 * xh;   // distance of this wave's first query
+    if constexpr (BIAS) {
+      if (__any(e0 > -far && e0 - 31 < far)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int x = min(max(e0 - c_row(r, g), -far), far) + far;
+          sm[r] = fast_exp2(fmaf(sm[r], sl2, bias[x]));
+        }
+      } else {
+        const float bc = bias[e0 < 0 ? 0 : 2 * far];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sm[r] = fast_exp2(fmaf(sm[r], sl2, bc));
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sm[r] = fast_exp2(sm[r] * sl2);
+    }
+    if (a.causal && __any(e0 > 0)) {   // queries before the key
+      int first = e0;
+      asm volatile("" : "+v"(first));
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (c_row(r, g) < first) sm[r] = 0.0f;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp[r] *= sm[r];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      *reinterpret_cast<bf16x8*>(smem + xw + (2 * u) * 1024) = c_to_operand(sm, u);
+      *reinterpret_cast<bf16x8*>(smem + xw + (2 * u + 1) * 1024) = c_to_operand(dp, u);
+    }
+    __syncthreads();   // P and dS of all 64 queries are there for both waves of the key half
+    bf16x8 pb[4], sb[4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      pb[ks] = lds_row(smem, xr + (2 * ks) * 1024);
+      sb[ks] = lds_row(smem, xr + (2 * ks + 1) * 1024);
+    }
+    sched_fence();
+#pragma unroll
+    for (int i = 0; i < NOP; ++i) {
+      const int ks = i / (2 * HT), dt = (i % (2 * HT)) / 2;
+      if (i % 2 == 0) dvT[dt] = mfma32(ta[i % PT], pb[ks], dvT[dt]);   // dO_i^T P
+      else dkT[dt] = mfma32(ta[i % PT], sb[ks], dkT[dt]);              // Q_i^T dS
+      if (i + PT < NOP) read_t(i + PT);
+      sched_fence();
+    }
+    if constexpr (BIAS) {
+      if (cur.i == ks_.i0 && s + 1 < s_end && a.G > 1) {   // the next step is of another head (its bias is read behind the next barrier)
+        __syncthreads();
+        expand_bias(a, cur.h, bias);
+      }
+    }
+  };
+  for (int s = s_beg; s < s_end; s += 2) {
+    step(s, 0);
+    if (s + 1 < s_end) step(s + 1, 1);
+  }
+  wait_vm0_known();        // the last step's surplus request has landed
+  if (cut) {
+    f32x4* o = key_slot<D>(kp, ((size_t)bh * kp.tiles + j) * kp.pieces + p, wu, l);
+#pragma unroll
+    for (int dt = 0; dt < HT; ++dt)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        o[(4 * dt + r4) * 64] = f32x4{dvT[dt][4 * r4], dvT[dt][4 * r4 + 1], dvT[dt][4 * r4 + 2], dvT[dt][4 * r4 + 3]};
+        o[(4 * (HT + dt) + r4) * 64] = f32x4{dkT[dt][4 * r4], dkT[dt][4 * r4 + 1], dkT[dt][4 * r4 + 2], dkT[dt][4 * r4 + 3]};
+      }
+    return;
+  }
+  __syncthreads();   // every wave is done with the tiles
+  store_keys<D>(a, gr, smem + wu * Lds::STG, dvT, dkT, b, hk, j, kh, xh, kok, l);
+}
+
+// dK, dV of the key tiles whose steps were cut: the sums of the pieces in order.  Bound by its traffic.
+template <int D>
+__global__ __launch_bounds__(256) void attn_kv_join_kernel(Attn a, AttnGrads gr, KeyPlan kp) {
+  constexpr int HT = D / 64, NQ = 2 * HT * 4;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, kh = w & 1, xh = w >> 1;
+  const int bh = blockIdx.x / kp.tiles, j = blockIdx.x - bh * kp.tiles, b = bh / a.Hkv, hk = bh - b * a.Hkv;
+  const Seq sq = seq_of(a, b);
+  const int total = key_steps(a, sq, j).total;
+  if (total <= kp.piece) return;
+  const int np = (total + kp.piece - 1) / kp.piece;
+  f32x4 s[NQ];
+  const size_t slot = (size_t)blockIdx.x * kp.pieces;
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) s[q] = key_slot<D>(kp, slot, w, l)[q * 64];
+  for (int e = 1; e < np; e += 2) {   // (two in flight; past the end: the last again, not added)
+    f32x4 x[2][NQ];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const f32x4* y = key_slot<D>(kp, slot + min(e + k, np - 1), w, l);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) x[k][q] = y[q * 64];
+    }
+    const bool two = e + 1 < np;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+      s[q] += x[0][q];
+      if (two) s[q] += x[1][q];
+    }
+  }
+  f32x16 dvT[HT], dkT[HT];
+#pragma unroll
+  for (int dt = 0; dt < HT; ++dt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      dvT[dt][r] = s[4 * dt + r / 4][r % 4];
+      dkT[dt][r] = s[4 * (HT + dt) + r / 4][r % 4];
+    }
+  store_keys<D>(a, gr, smem + wave_uniform(w) * DkLds<D>::STG, dvT, dkT, b, hk, j, kh, xh,
+                j * kBlk + kh * 32 + (l & 31) < sq.nk, l);
+}
+
+struct BwdPlan {
+  KeyPlan key;
+  float *Ds, *tpart;
+  int qtiles;
+  size_t bytes;
+};
+
+// Key tiles alone may not fill the chip (text of a few hundred tokens under a long video), and under a causal mask the
+// first one has all queries and the last one few.  A piece costs about ten steps beside its own (operands, sums out
+// and back, the joining launch); among its numbers the least estimated time is taken, in steps: full rounds of the
+// chip's workgroups where all tiles are alike, average and one last piece where they are not.
+BwdPlan plan_of(const Attn& a, char* ws) {
+  BwdPlan p = {};
+  size_t off = 0;
+  auto take = [&](size_t n) {
+    float* x = reinterpret_cast<float*>(ws + off);
+    off += align_up(n * sizeof(float));
+    return x;
+  };
+  p.qtiles = (a.Nq + kBlk - 1) / kBlk;
+  KeyPlan& k = p.key;
+  k.tiles = (a.Nk + kBlk - 1) / kBlk;
+  k.blocks = k.tiles ? block_row(k.tiles) * block_rows(a.B * a.Hkv, k.tiles) : 0;
+  const double slots = a.d == 64 ? 768 : 512, units = (double)a.B * a.Hkv * k.tiles, steps = (double)a.G * p.qtiles;
+  double best = 1e300;
+  k.pieces = 1;
+  for (int n = 1; n <= 64 && n <= steps; ++n) {
+    const double len = ceil(steps / n), extra = n > 1 ? 10.0 : 4.0;
+    const double t = a.causal ? (0.5 * units * steps + (n > 1 ? 0.5 * n + 0.5 : 1.0) * units * extra) / slots + len
+                              : ceil(units * n / slots) * (len + extra);
+    if (t < 0.95 * best) {
+      best = t;
+      k.pieces = n;
+    }
+  }
+  k.piece = k.pieces > 1 ? (int)ceil(steps / k.pieces) : 0x7fffffff;
+  p.Ds = take((size_t)a.B * a.H * a.Nq);
+  p.tpart = take(a.has_bias() ? (size_t)a.B * a.H * p.qtiles * bucket_count(a.bias) : 0);
+  k.part = take(k.pieces > 1 ? (size_t)units * k.pieces * 2 * kBlk * a.d : 0);
+  p.bytes = off;
+  return p;
+}
+
+template <int D>
+hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
+  const BwdPlan p = plan_of(a, ws);
+  {
+    const int lds = DqLds<D>::FIXED + (a.has_bias() ? dq_bias_lds(a.bias.far) : 0);
+    auto kern = a.has_bias() ? attn_dq_kernel<D, true> : attn_dq_kernel<D, false>;
+    SLA_TRY(ensure_dyn_lds(kern, lds));
+    KernelTimer kt("attn_dq", st);
+    kern<<<dim3(block_row(p.qtiles), block_rows(a.B * a.H, p.qtiles)), 256, lds, st>>>(a, g, p.Ds, p.tpart, p.qtiles);
+  }
+  const int tables = g.dtable ? a.H : 0, grid = p.key.blocks * p.key.pieces + tables;
+  if (grid == 0) return hipGetLastError();
+  {
+    const int lds = DkLds<D>::BIAS + (a.has_bias() ? (2 * a.bias.far + 1) * 4 : 0);
+    auto kern = a.has_bias() ? attn_dkdv_kernel<D, true> : attn_dkdv_kernel<D, false>;
+    SLA_TRY(ensure_dyn_lds(kern, lds));
+    KernelTimer kt("attn_dkdv", st);
+    kern<<<grid, 256, lds, st>>>(a, g, p.Ds, p.key, p.tpart, p.qtiles);
+  }
+  if (p.key.pieces > 1) {
+    KernelTimer kt("attn_kv_join", st);
+    attn_kv_join_kernel<D><<<a.B * a.Hkv * p.key.tiles, 256, 4 * DkLds<D>::STG, st>>>(a, g, p.key);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_backward_ws_bf16(const Attn& a) { return plan_of(a, nullptr).bytes; }
+
+hipError_t attn_backward_bf16(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
+  return a.d == 64 ? backward_impl<64>(a, g, ws, st) : backward_impl<128>(a, g, ws, st);
+}
+
+}  // namespace sla

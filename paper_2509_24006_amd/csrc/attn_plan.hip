@@ -154,4 +154,10 @@ hipError_t attn_forward(const Attn& a, char* ws, hipStream_t st) {
   return attn_forward_bf16(a, attn_plan(a, ws), st);
 }
 
+size_t attn_backward_ws(const Attn& a) { return a.dtype == SLA_F32 ? attn_backward_ws_f32(a) : attn_backward_ws_bf16(a); }
+
+hipError_t attn_backward(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
+  return a.dtype == SLA_F32 ? attn_backward_f32(a, g, ws, st) : attn_backward_bf16(a, g, ws, st);
+}
+
 }  // namespace sla

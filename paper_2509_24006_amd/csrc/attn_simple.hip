@@ -210,16 +210,14 @@ hipError_t backward_impl(const Attn& a, const AttnGrads& g, float* Ds, hipStream
 
 }  // namespace
 
-size_t attn_backward_ws(const Attn& a) { return align_up((size_t)a.B * a.H * a.Nq * 4); }
+size_t attn_backward_ws_f32(const Attn& a) { return align_up((size_t)a.B * a.H * a.Nq * 4); }
 
 hipError_t attn_forward_f32(const Attn& a, hipStream_t st) {
   return a.d == 64 ? forward_impl<float, 64>(a, st) : forward_impl<float, 128>(a, st);
 }
-hipError_t attn_backward(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
+hipError_t attn_backward_f32(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
   float* Ds = reinterpret_cast<float*>(ws);
-  if (a.dtype == SLA_F32)
-    return a.d == 64 ? backward_impl<float, 64>(a, g, Ds, st) : backward_impl<float, 128>(a, g, Ds, st);
-  return a.d == 64 ? backward_impl<__hip_bfloat16, 64>(a, g, Ds, st) : backward_impl<__hip_bfloat16, 128>(a, g, Ds, st);
+  return a.d == 64 ? backward_impl<float, 64>(a, g, Ds, st) : backward_impl<float, 128>(a, g, Ds, st);
 }
 
 }  // namespace sla
