@@ -69,10 +69,7 @@ bool attn_forward_fits(const Attn& a);   // whether offsets inside the tensors f
 hipError_t attn_forward(const Attn& a, char* ws, hipStream_t st);
 hipError_t attn_backward(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st);
 
-// the same by storage type
-hipError_t attn_forward_f32(const Attn& a, hipStream_t st);
-size_t attn_backward_ws_f32(const Attn& a);
-size_t attn_backward_ws_bf16(const Attn& a);
+// the backward pass by storage type
 hipError_t attn_backward_f32(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st);
 hipError_t attn_backward_bf16(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st);
 

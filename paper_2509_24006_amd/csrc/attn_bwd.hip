@@ -8,7 +8,7 @@
 // P and dS enter their second products rounded to bf16, the matrix cores' operand type; all sums are in float.
 #include <math.h>
 
-#include "attn.h"
+#include "attn_bwd.h"
 #include "mfma_common.h"
 
 namespace sla {
@@ -211,6 +211,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, A
     step(j, 0);
     if (j + 1 < steps) step(j + 1, 1);
   }
+  if constexpr (BIAS) table_part<8>(a, dist, width, sumL, sumR, tpart + ((size_t)bh * tiles + i) * bucket_count(a.bias));
   // ---- add the two key halves in a row-major staging area, then every thread stores 8-byte pieces of whole rows
   __syncthreads();   // every wave is done with the tiles
   constexpr int C4 = D / 4, NIT = kBlk * C4 / 256, SP = Lds::SP;
@@ -224,24 +225,6 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, A
         *reinterpret_cast<f32x4*>(stg + srow + 32 * dt + 8 * r4) =
             f32x4{dqT[dt][4 * r4], dqT[dt][4 * r4 + 1], dqT[dt][4 * r4 + 2], dqT[dt][4 * r4 + 3]};
   }
-  if constexpr (BIAS) {
-    // the far sums of the four waves, and the eight arrays into the first
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-      sumL += __shfl_xor(sumL, o);
-      sumR += __shfl_xor(sumR, o);
-    }
-    if (l == 0) {
-      dist[8 * width + w] = sumL;
-      dist[8 * width + 4 + w] = sumR;
-    }
-    for (int x = tid; x < width; x += 256) {
-      float t = dist[x];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) t += dist[e * width + x];
-      dist[x] = t;
-    }
-  }
   __syncthreads();
   if (kh == 0) {
 #pragma unroll
@@ -253,26 +236,6 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, A
         for (int r = 0; r < 4; ++r) x[r] = live ? x[r] + dqT[dt][4 * r4 + r] : 0.0f;
         *reinterpret_cast<f32x4*>(stg + srow + 32 * dt + 8 * r4) = x;
       }
-  }
-  if constexpr (BIAS) {
-    // bucket by bucket: the distances [n0, n1) of a side, the last bucket with the far sum
-    const int nb = bucket_count(a.bias), side = a.bias.n_borders + 1;
-    if (tid >= 256 - nb) {
-      const int u = 255 - tid, v = u >= side ? u - side : u;
-      const bool right = u >= side;
-      const int n0 = v ? a.bias.borders[v - 1] : 0, n1 = v < side - 1 ? a.bias.borders[v] : far;
-      float t = 0.0f;
-      for (int x = n0; x < n1; ++x)
-        if (!right || x > 0) t += dist[right ? far + x : far - x];
-      const float* e = dist + 8 * width + (right ? 4 : 0);
-      const float sr = (dist[8 * width + 4] + dist[8 * width + 5]) + (dist[8 * width + 6] + dist[8 * width + 7]);
-      if (v == side - 1) t += (e[0] + e[1]) + (e[2] + e[3]);
-      if (!a.bias.two_sided && v == 0) {   // keys behind the query
-        for (int x = 1; x < far; ++x) t += dist[far + x];
-        t += sr;
-      }
-      tpart[((size_t)bh * tiles + i) * nb + u] = t;
-    }
   }
   __syncthreads();
   bf16* const dQ = reinterpret_cast<bf16*>(gr.dQ.p) + (size_t)b * gr.dQ.sb + (size_t)h * gr.dQ.sh + (size_t)q0 * gr.dQ.sn;
@@ -286,31 +249,6 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, A
       for (int r = 0; r < 4; ++r) pk[r] = (__bf16)(sv[r] * a.scale);
       *reinterpret_cast<bf16x4*>(dQ + (size_t)row * gr.dQ.sn + 4 * c4) = pk;
     }
-  }
-}
-
-// The gradient of one head's column of the table: the sum of the parts [b][tile], in an order fixed by their number.
-__device__ __forceinline__ void table_sum(const Attn& a, const AttnGrads& gr, const float* tpart, int tiles, int h,
-                                          unsigned char* smem) {
-  float* red = reinterpret_cast<float*>(smem);   // [slice][nb]
-  const int nb = bucket_count(a.bias), slices = 256 / nb, u = threadIdx.x % nb, sl = threadIdx.x / nb;
-  const int total = a.B * tiles;
-  if (sl < slices) {
-    float s = 0.0f;
-#pragma unroll 4
-    for (int x = sl; x < total; x += slices) {
-      const int b = x / tiles, t = x - b * tiles;
-      s += tpart[(((size_t)b * a.H + h) * tiles + t) * nb + u];
-    }
-    red[sl * nb + u] = s;
-  }
-  __syncthreads();
-  if ((int)threadIdx.x < nb) {
-    float s = 0.0f;
-    for (int x = 0; x < slices; ++x) s += red[x * nb + threadIdx.x];
-    const size_t at = (size_t)threadIdx.x * a.H + h;
-    if (a.table16) reinterpret_cast<__bf16*>(gr.dtable)[at] = (__bf16)s;
-    else reinterpret_cast<float*>(gr.dtable)[at] = s;
   }
 }
 
@@ -330,23 +268,6 @@ struct DkLds {
   static constexpr int STG = 32 * (64 * (D / 64) + 16);  // output staging of one wave, laid over the tiles
 };
 
-// The steps of a key tile run over the query tiles from the first that sees it, head by head.  Above `piece` of them they
-// are cut: piece p leaves its sums in slot unit * pieces + p, and attn_kv_join adds them.
-struct KeyPlan {
-  int tiles, pieces, piece;   // key tiles; most pieces of one, steps in a piece
-  float* part;                // [B Hkv tiles][pieces] slots of 2 x 64 x d floats
-  int blocks;                 // workgroups of one piece index
-};
-struct KeySteps {
-  int i0, per_head, total;    // first query tile, tiles per head, steps
-};
-__device__ __forceinline__ KeySteps key_steps(const Attn& a, const Seq& s, int j) {
-  KeySteps k;
-  k.i0 = a.causal ? max(0, j * kBlk - s.pos) / kBlk : 0;
-  k.per_head = j * kBlk < s.nk ? max(0, (s.nq + kBlk - 1) / kBlk - k.i0) : 0;
-  k.total = k.per_head * a.G;
-  return k;
-}
 template <int D>
 __device__ __forceinline__ f32x4* key_slot(const KeyPlan& kp, size_t slot, int w, int l) {
   return reinterpret_cast<f32x4*>(kp.part + slot * (2 * kBlk * D)) + w * (D / 8 * 64) + l;
@@ -653,52 +574,9 @@ __global__ __launch_bounds__(256) void attn_kv_join_kernel(Attn a, AttnGrads gr,
                 j * kBlk + kh * 32 + (l & 31) < sq.nk, l);
 }
 
-struct BwdPlan {
-  KeyPlan key;
-  float *Ds, *tpart;
-  int qtiles;
-  size_t bytes;
-};
-
-// Key tiles alone may not fill the chip (text of a few hundred tokens under a long video), and under a causal mask the
-// first one has all queries and the last one few.  A piece costs about ten steps beside its own (operands, sums out
-// and back, the joining launch); among its numbers the least estimated time is taken, in steps: full rounds of the
-// chip's workgroups where all tiles are alike, average and one last piece where they are not.
-BwdPlan plan_of(const Attn& a, char* ws) {
-  BwdPlan p = {};
-  size_t off = 0;
-  auto take = [&](size_t n) {
-    float* x = reinterpret_cast<float*>(ws + off);
-    off += align_up(n * sizeof(float));
-    return x;
-  };
-  p.qtiles = (a.Nq + kBlk - 1) / kBlk;
-  KeyPlan& k = p.key;
-  k.tiles = (a.Nk + kBlk - 1) / kBlk;
-  k.blocks = k.tiles ? block_row(k.tiles) * block_rows(a.B * a.Hkv, k.tiles) : 0;
-  const double slots = a.d == 64 ? 768 : 512, units = (double)a.B * a.Hkv * k.tiles, steps = (double)a.G * p.qtiles;
-  double best = 1e300;
-  k.pieces = 1;
-  for (int n = 1; n <= 64 && n <= steps; ++n) {
-    const double len = ceil(steps / n), extra = n > 1 ? 10.0 : 4.0;
-    const double t = a.causal ? (0.5 * units * steps + (n > 1 ? 0.5 * n + 0.5 : 1.0) * units * extra) / slots + len
-                              : ceil(units * n / slots) * (len + extra);
-    if (t < 0.95 * best) {
-      best = t;
-      k.pieces = n;
-    }
-  }
-  k.piece = k.pieces > 1 ? (int)ceil(steps / k.pieces) : 0x7fffffff;
-  p.Ds = take((size_t)a.B * a.H * a.Nq);
-  p.tpart = take(a.has_bias() ? (size_t)a.B * a.H * p.qtiles * bucket_count(a.bias) : 0);
-  k.part = take(k.pieces > 1 ? (size_t)units * k.pieces * 2 * kBlk * a.d : 0);
-  p.bytes = off;
-  return p;
-}
-
 template <int D>
 hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
-  const BwdPlan p = plan_of(a, ws);
+  const BwdPlan p = attn_bwd_plan(a, ws);
   {
     const int lds = DqLds<D>::FIXED + (a.has_bias() ? dq_bias_lds(a.bias.far) : 0);
     auto kern = a.has_bias() ? attn_dq_kernel<D, true> : attn_dq_kernel<D, false>;
@@ -723,8 +601,6 @@ hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_
 }
 
 }  // namespace
-
-size_t attn_backward_ws_bf16(const Attn& a) { return plan_of(a, nullptr).bytes; }
 
 hipError_t attn_backward_bf16(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
   return a.d == 64 ? backward_impl<64>(a, g, ws, st) : backward_impl<128>(a, g, ws, st);

@@ -13,9 +13,7 @@
 // rounded to bf16 (the matrix cores' operand); its sum is taken before the rounding, in float.
 #include <type_traits>
 
-#include "attn.h"
-#include "attn_plan.h"
-#include "mfma_common.h"
+#include "attn_rows.h"
 
 namespace sla {
 namespace {
@@ -30,30 +28,6 @@ struct AttnLds {
   static constexpr int BIAS = ROWO + 256;       // per head of the tile 2 far + 1 floats: bias in log2 units by distance
 };
 
-// The query of a row, from its index in the unit's rows.
-struct RowOf {
-  int b, g, n;
-  bool in;
-};
-__device__ __forceinline__ RowOf row_of(const Attn& a, const AttnPart& pt, int unit_b, int r) {
-  RowOf o;
-  o.in = r < pt.rows;
-  o.b = unit_b;
-  o.g = 0;
-  o.n = r;
-  if (pt.packed) {
-    const int rg = r / a.Nq;
-    o.n = r - rg * a.Nq;
-    o.g = rg;
-    if (unit_b < 0) {   // rows of all sequences
-      o.b = rg / pt.heads;
-      o.g = rg - o.b * pt.heads;
-    }
-  }
-  if (!o.in) o.b = o.g = o.n = 0;
-  return o;
-}
-
 // PART: the workgroup leaves sums for attn_join_kernel.
 template <int D, bool BIAS, bool PART>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan, float c2) {
@@ -64,64 +38,23 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 5, ln = l & 31;
   const int qh = w & 1, par = w >> 1;
 
-  // ---- which rows and keys
-  const bool pre = PART && (int)blockIdx.x < plan.prefix.blocks;   // a tile of the shared prefix
-  const AttnPart& pt = pre ? plan.prefix : plan.own;
-  int unit, tile, part = 0;
-  if constexpr (PART) {
-    int x = blockIdx.x - (pre ? 0 : plan.prefix.blocks);
-    part = x % pt.splits;   // (parts of a unit next to each other: an XCD gets every eighth of them)
-    x /= pt.splits;
-    tile = x % pt.tiles;
-    unit = x / pt.tiles;
-  } else {
-    const BlockOf own = block_of(blockIdx.y, blockIdx.x, plan.own.units, plan.own.tiles);
-    if (own.i < 0) return;
-    unit = own.bh;
-    tile = a.causal ? plan.own.tiles - 1 - own.i : own.i;   // (longest rows first)
-  }
-  unit = wave_uniform(unit);
-  tile = wave_uniform(tile);
-  const int per_b = a.H / pt.heads;                        // units per sequence (prefix: units in all)
-  const int ub = pre ? -1 : unit / per_b, uh = pre ? unit : unit - ub * per_b;
-  const int h0 = uh * pt.heads, hk = h0 / a.G;             // first query head, K, V head
-  const int r0 = tile * kBlk;
-  int limmax;                                              // keys that any row of the tile may see
-  if (pre) {
-    limmax = a.Np;
-  } else {
-    const Seq s = seq_of(a, ub);
-    const int last = pt.packed ? s.nq : min(r0 + kBlk, s.nq);   // one behind the last query
-    limmax = (pt.packed ? s.nq > 0 : last > r0) ? s.nk : 0;
-    if (a.causal) limmax = max(0, min(limmax, s.pos + last - a.Np));
-  }
-  const int T_all = (limmax + kBlk - 1) / kBlk;
-  const int t0 = PART ? (int)((long long)T_all * part / pt.splits) : 0;
-  const int t1 = PART ? (int)((long long)T_all * (part + 1) / pt.splits) : T_all;
-  const int steps = wave_uniform(t1 - t0);
-
-  // ---- this lane's row
-  const RowOf row = row_of(a, pt, ub, r0 + qh * 32 + ln);
-  const Seq seq = seq_of(a, row.b);
-  const bool live = row.in && row.n < seq.nq;
-  const int base_pos = pre ? 0 : a.Np;
-  const int posk = seq.pos + row.n - base_pos;             // the row's position, counted in this part's keys
-  // keys of this part that the row sees; rows that are not live see all they come across, and are written as zeros
-  int lim = 0x7fffffff;
-  if (live) {
-    lim = pre ? a.Np : seq.nk;
-    if (a.causal) lim = max(0, min(lim, posk + 1));
-  }
-  const size_t qbase = (size_t)(ub < 0 ? 0 : ub) * a.Q.sb + (size_t)h0 * a.Q.sh + (pt.packed ? 0 : (size_t)r0 * a.Q.sn);
-  const size_t obase = (size_t)(ub < 0 ? 0 : ub) * a.O.sb + (size_t)h0 * a.O.sh + (pt.packed ? 0 : (size_t)r0 * a.O.sn);
+  FwdTile x;
+  if (!x.template open<PART>(a, plan)) return;
+  const AttnPart& pt = x.pre ? plan.prefix : plan.own;
+  const int steps = x.steps, h0 = x.h0;
+  const RowOf row = x.row(a, pt, qh * 32 + ln);   // this lane's
+  const RowKeys rk = row_keys(a, x, row);
+  const bool live = rk.live;
+  const int posk = rk.pos, lim = rk.lim;
+  // 32-bit offsets of the tile's rows, from the unit's first row or, where a unit is one head, the tile's
+  RowOf first = {max(x.ub, 0), 0, pt.packed ? 0 : x.r0, true};
+  const long long qbase = x.at(a.Q, first), obase = x.at(a.O, first);
   int* const rowq = reinterpret_cast<int*>(smem + Lds::ROWQ);
   int* const rowo = reinterpret_cast<int*>(smem + Lds::ROWO);
   if (tid < kBlk) {
-    const RowOf x = row_of(a, pt, ub, r0 + tid);
-    const int n = pt.packed ? x.n : x.n - r0;
-    const long long bq = ub < 0 ? (long long)x.b * a.Q.sb : 0, bo = ub < 0 ? (long long)x.b * a.O.sb : 0;
-    rowq[tid] = x.in && x.n < seq_of(a, x.b).nq ? (int)(2 * (bq + (long long)x.g * a.Q.sh + (long long)n * a.Q.sn)) : -1;
-    rowo[tid] = x.in ? (int)((bo + (long long)x.g * a.O.sh + (long long)n * a.O.sn) >> 3) : -1;
+    const RowOf r = x.row(a, pt, tid);
+    rowq[tid] = r.in && r.n < seq_of(a, r.b).nq ? (int)(2 * (x.at(a.Q, r) - qbase)) : -1;
+    rowo[tid] = r.in ? (int)((x.at(a.O, r) - obase) >> 3) : -1;
   }
   float* const bias = reinterpret_cast<float*>(smem + Lds::BIAS);
   const int far = a.bias.far, width = 2 * far + 1;
@@ -137,16 +70,14 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
 #pragma unroll
   for (int et = 0; et < NT; ++et) oT[et] = zero_f32x16();
   float m = -INFINITY, lsum = 0.0f;
-  const View &VK = pre ? a.Kp : a.K, &VV = pre ? a.Vp : a.V;
+  const View &VK = x.pre ? a.Kp : a.K, &VV = x.pre ? a.Vp : a.V;
   RunLoader<D> tk, tv;
   tk.init(lds_base(smem), w, l, 2 * VK.sn, kBlk);
   tv.init(lds_base(smem), w, l, 2 * VV.sn, kBlk);
   constexpr int IPW = RunLoader<D>::IPW;
   // the descriptors span this workgroup's keys up to the last valid one: rows behind it read as zeros
-  const int keys = max(1, min(limmax, t1 * kBlk) - t0 * kBlk);
   auto rsrc = [&](const View& v) {
-    const bf16* p = reinterpret_cast<const bf16*>(v.p) + (size_t)(pre ? 0 : ub) * v.sb + (size_t)hk * v.sh + (size_t)t0 * kBlk * v.sn;
-    return tile_rsrc(p, (keys - 1) * 2 * v.sn + 2 * D);
+    return tile_rsrc(reinterpret_cast<const bf16*>(v.p) + x.key_at(v), (x.keys() - 1) * 2 * v.sn + 2 * D);
   };
   const BufDesc descK = rsrc(VK), descV = rsrc(VV);
   constexpr int QSLOT = 3 * Lds::TILE;
@@ -218,7 +149,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   }
   const float cs = BIAS ? 1.0f : c2;              // the scores' factor in the exponent of 2
   const float* const brow = bias + (BIAS ? row.g * width : 0);
-  int key0 = t0 * kBlk + 32 * wave_uniform(par);  // first key of this wave in the current tile
+  int key0 = x.t0 * kBlk + 32 * wave_uniform(par);  // first key of this wave in the current tile
   int koff = 3 * tk.tile_step, voff = 2 * tv.tile_step;
   // One step; P = parity of s.  On entry K_{s+1} and V_s are in their slots for every wave and sT holds S_s; sN
   // receives S_{s+1}.  The wave copies its operands to registers first; a second barrier then frees both slots for
@@ -364,7 +295,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   f32x16 (&o)[HT] = *reinterpret_cast<f32x16 (*)[HT]>(&oT[0]);
   if constexpr (PART) {
     // rows of D floats, and (maximum in log2 units, sum) of every row; without a key the sum is 0 and the row is not read
-    const size_t slot = (size_t)pt.slot0 + ((size_t)unit * pt.tiles + tile) * pt.splits + part;
+    const size_t slot = x.slot(pt);
     if (row.in) {
       const int r = qh * 32 + ln;
       float* const po = plan.part + (slot * kBlk + r) * D + (par ? D / 2 : 0) + 4 * g;

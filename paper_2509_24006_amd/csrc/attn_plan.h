@@ -1,4 +1,4 @@
-// How a forward pass is cut into workgroups (attn_plan.hip).
+// How a forward pass is cut into workgroups.
 #ifndef SLA_ATTN_PLAN_H_
 #define SLA_ATTN_PLAN_H_
 
@@ -25,6 +25,7 @@ size_t attn_plan_ws(const Attn& a, const AttnPlan& p);
 
 hipError_t attn_join(const Attn& a, const AttnPlan& plan, hipStream_t st);
 hipError_t attn_forward_bf16(const Attn& a, const AttnPlan& plan, hipStream_t st);
+hipError_t attn_forward_f32(const Attn& a, const AttnPlan& plan, hipStream_t st);
 
 }  // namespace sla
 #endif

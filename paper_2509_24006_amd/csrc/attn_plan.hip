@@ -1,8 +1,11 @@
-// Plan of a forward pass, and the kernel that joins the sums of keys that were cut.
+// How the passes are cut into workgroups, and the kernel that joins the forward pass's sums of keys that were cut.
 #include "attn_plan.h"
+
+#include <math.h>
 
 #include <algorithm>
 
+#include "attn_bwd.h"
 #include "mfma_common.h"
 
 namespace sla {
@@ -147,15 +150,53 @@ hipError_t attn_join(const Attn& a, const AttnPlan& plan, hipStream_t st) {
   return hipGetLastError();
 }
 
-size_t attn_forward_ws(const Attn& a) { return a.dtype == SLA_F32 ? 0 : attn_plan_ws(a, attn_plan(a, nullptr)); }
-
-hipError_t attn_forward(const Attn& a, char* ws, hipStream_t st) {
-  if (a.dtype == SLA_F32) return attn_forward_f32(a, st);
-  return attn_forward_bf16(a, attn_plan(a, ws), st);
+// Key tiles alone may not fill the chip (text of a few hundred tokens under a long video), and under a causal mask the
+// first one has all queries and the last one few.  A piece costs about ten steps beside its own (operands, sums out and
+// back, the joining launch; float steps are longer, there it is three); among the numbers of pieces the least estimated
+// time is taken, in steps: full rounds of the chip's workgroups where all tiles are alike, average and one last
+// piece where they are not.
+BwdPlan attn_bwd_plan(const Attn& a, char* ws) {
+  BwdPlan p = {};
+  size_t off = 0;
+  auto take = [&](size_t n) {
+    float* x = reinterpret_cast<float*>(ws + off);
+    off += align_up(n * sizeof(float));
+    return x;
+  };
+  const bool f32 = a.dtype == SLA_F32;
+  p.qtiles = (a.Nq + kBlk - 1) / kBlk;
+  KeyPlan& k = p.key;
+  k.tiles = (a.Nk + kBlk - 1) / kBlk;
+  const long long units = (long long)a.B * a.Hkv * k.tiles;
+  k.quarters = f32 ? (units < 384 ? 4 : 2) : 1;
+  k.blocks = units == 0 ? 0 : f32 ? (int)units * k.quarters : block_row(k.tiles) * block_rows(a.B * a.Hkv, k.tiles);
+  const double slots = !f32 && a.d == 64 ? 768 : 512, wgs = (double)units * k.quarters, steps = (double)a.G * p.qtiles;
+  double best = 1e300;
+  k.pieces = 1;
+  for (int n = 1; n <= 64 && n <= steps; ++n) {
+    const double len = ceil(steps / n), extra = n == 1 ? 3.0 : f32 ? 4.0 : 10.0;
+    const double t = a.causal ? (0.5 * wgs * steps + (n > 1 ? 0.5 * n + 0.5 : 1.0) * wgs * extra) / slots + len
+                              : ceil(wgs * n / slots) * (len + extra);
+    if (t < 0.95 * best) {
+      best = t;
+      k.pieces = n;
+    }
+  }
+  k.piece = k.pieces > 1 ? (int)ceil(steps / k.pieces) : 0x7fffffff;
+  p.Ds = take((size_t)a.B * a.H * a.Nq);
+  p.tpart = take(a.has_bias() ? (size_t)a.B * a.H * p.qtiles * bucket_count(a.bias) : 0);
+  k.part = take(k.pieces > 1 ? (size_t)units * k.pieces * 2 * kBlk * a.d : 0);
+  p.bytes = off;
+  return p;
 }
 
-size_t attn_backward_ws(const Attn& a) { return a.dtype == SLA_F32 ? attn_backward_ws_f32(a) : attn_backward_ws_bf16(a); }
+size_t attn_forward_ws(const Attn& a) { return attn_plan_ws(a, attn_plan(a, nullptr)); }
+size_t attn_backward_ws(const Attn& a) { return attn_bwd_plan(a, nullptr).bytes; }
 
+hipError_t attn_forward(const Attn& a, char* ws, hipStream_t st) {
+  const AttnPlan p = attn_plan(a, ws);
+  return a.dtype == SLA_F32 ? attn_forward_f32(a, p, st) : attn_forward_bf16(a, p, st);
+}
 hipError_t attn_backward(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
   return a.dtype == SLA_F32 ? attn_backward_f32(a, g, ws, st) : attn_backward_bf16(a, g, ws, st);
 }
