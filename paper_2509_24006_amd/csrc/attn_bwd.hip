@@ -6,7 +6,7 @@
 // S and dP are formed in both kernels (seven products instead of five): dQ summed where dK and dV are would need float
 // atomics of a 64 x d tile per pair, whose order changes the result and whose traffic costs more than the two products.
 // P and dS enter their second products rounded to bf16, the matrix cores' operand type; all sums are in float.
-#include <math.h>
+#include <type_traits>
 
 #include "attn_bwd.h"
 #include "mfma_common.h"
@@ -32,20 +32,29 @@ struct DqLds {
   static constexpr int BUF = 2 * TILE;             // K_j and V_j
   static constexpr int SP = D + 4;                 // floats per row of the output staging
   static constexpr int FIXED = 2 * BUF > kBlk * SP * 4 ? 2 * BUF : kBlk * SP * 4;
-  // with a bias: the bias by distance, then the sums of dS by distance, one array per wave and lane half
-  static constexpr int BIAS = FIXED;
+  static constexpr int STAT = FIXED;               // a sum of each of the 64 queries and two key halves
+  // with a bias: 16 x 32 floats per wave, the bias by distance, the sums of dS by distance (an array per wave)
+  static constexpr int SKEW = STAT + 512;
+  static constexpr int BIAS = SKEW + 4 * 2048;
 };
-__host__ __device__ inline int dq_bias_lds(int far) { return 9 * (2 * far + 1) * 4 + 32; }
+template <int D>
+int dq_lds(const Attn& a) { return a.has_bias() ? DqLds<D>::BIAS + 5 * (2 * a.bias.far + 1) * 4 + 32 : DqLds<D>::SKEW; }
 
 // Wave (qh, kh): S^T and dP^T are [key][query], one query per lane, so L and D are per-lane scalars and dS^T feeds
 // dQ^T = K^T dS^T from registers.  The two kh waves hold sums over their keys and are added at the end.
 //
+// D: rowsum(dO O) has the rounding of O in it, which a sum of dS over many keys of a row (the last bucket of a bias) does not
+// average out, nor a row with few keys.  The sum of P (dP - D') over all keys is D - D' whatever D' is: the key side gets the
+// D that is corrected by it, and the last buckets' sums are corrected too.  dQ takes D' = rowsum(dO O) where there are
+// many keys, and otherwise (up to two tiles) D from a pass over them before.
+//
 // The table's gradient is a sum of dS by distance.  Away from the diagonal a lane's values all belong to the last bucket
-// of a side, and stay in a register; near it a value is added in LDS at its distance.  The 32 lanes of a half hold
-// consecutive queries, so the distances of one instruction differ, and every half of every wave has an array of its own:
-// the order of the additions is fixed.
+// of a side, and stay in registers.  Near it the wave's 32 x 32 values are summed along their diagonals through LDS, 16 keys
+// at a time: lane e reads the values of the diagonals e and e - 32.  A wave meets a distance in one step only (its
+// distances move on by 64 and span 63), so that the sum is stored, not added: no atomics, which take a cycle per lane.
+// (768 workgroups of up to 8 steps: 64 us with LDS atomics, 32 this way.)
 template <int D, bool BIAS>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, AttnGrads gr, float* __restrict__ Ds,
+__global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(Attn a, AttnGrads gr, float* __restrict__ Ds,
                                                                         float* __restrict__ tpart, int tiles) {
   using Lds = DqLds<D>;
   using T = SwzTile<D>;
@@ -85,11 +94,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, A
   }
   float* const bias = reinterpret_cast<float*>(smem + Lds::BIAS);
   const int far = a.bias.far, width = 2 * far + 1;
-  float* const dist = bias + width;                    // [wave][half][width]
-  float* const mine = dist + (2 * w + g) * width;
+  float* const dist = bias + width;                    // [wave][width]
+  float* const skew = reinterpret_cast<float*>(smem + Lds::SKEW) + 512 * w;
+  float* const stat = reinterpret_cast<float*>(smem + Lds::STAT);   // [kh][64]
   if constexpr (BIAS) {
     expand_bias(a, h, bias);
-    for (int x = tid; x < 8 * width; x += 256) dist[x] = 0.0f;
+    for (int x = tid; x < 4 * width; x += 256) dist[x] = 0.0f;
   }
   wait_vm0_known();
   __syncthreads();
@@ -118,42 +128,50 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, A
     for (int e = 0; e < 8; ++e) dsum = fmaf((float)gf[t][e], (float)of[t][e], dsum);
   }
   dsum = live ? half_sum(dsum) : 0.0f;
-  if (kh == 0 && g == 0 && live) Ds[li] = dsum;
-  const float nDq = -dsum;
+  float nDq = -dsum, drow = 0.0f;   // drow: sum of P (dP - D') over this lane's keys
   f32x16 dqT[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) dqT[t] = zero_f32x16();
   float sumL = 0.0f, sumR = 0.0f;   // dS at distances of -far and less, far and more
+  float pL = 0.0f, pR = 0.0f;       // P there (in tiles that lie there as a whole)
   TileAddr<D> ad;   // this wave reads rows 32 kh .. of K_j and V_j
   ad.init(32 * kh, l);
-  auto step = [&](int j, const int buf) __attribute__((always_inline)) {
+  // MAIN: the step proper; else only drow
+  auto step = [&](auto Main, int j, const int buf) __attribute__((always_inline)) {
+    constexpr bool MAIN = decltype(Main)::value;
     const int KO = buf * Lds::BUF, VO = KO + Lds::TILE;
     const int key0 = j * kBlk + 32 * wave_uniform(kh);
     ad.refresh();
     wait_vm0();
     __syncthreads();   // tiles of step j have landed for every wave; step j - 1 is fully consumed
     if (j + 1 < steps) issue(j + 1, buf ^ 1);
-    bf16x8 ka[KT], va[KT], ta[2][NT];
+    constexpr int PF = 4;   // LDS reads run PF operand pairs ahead of the products
+    bf16x8 ka[PF], va[PF], ta[2][NT];
+    auto read_s = [&](int t) __attribute__((always_inline)) {
+      ka[t % PF] = lds_row(smem, ad.row(t) + KO);
+      va[t % PF] = lds_row(smem, ad.row(t) + VO);
+    };
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      ka[t] = lds_row(smem, ad.row(t) + KO);
-      va[t] = lds_row(smem, ad.row(t) + VO);
-    }
+    for (int t = 0; t < PF; ++t) read_s(t);
     sched_fence();
-    f32x16 sT = zero_f32x16(), dpT;   // (dP starts at -D of the lane's query)
+    f32x16 sT = zero_f32x16(), dpT;   // (dP starts at -D' of the lane's query)
 #pragma unroll
     for (int r = 0; r < 16; ++r) dpT[r] = nDq;
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
-      sT = mfma32(ka[t], qf[t], sT);
-      dpT = mfma32(va[t], gf[t], dpT);
+      sT = mfma32(ka[t % PF], qf[t], sT);
+      dpT = mfma32(va[t % PF], gf[t], dpT);
+      if (t + PF < KT) read_s(t + PF);
+      sched_fence();
     }
     // K_j^T for the third product arrives under the exponentials
+    if constexpr (MAIN) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int dt = 0; dt < NT; ++dt)
-        ta[u][dt] = lds_tr<D>(smem, ad.tr(0, dt) + KO + u * RB, ad.tr(1, dt) + KO + u * RB);
+        for (int dt = 0; dt < NT; ++dt)
+          ta[u][dt] = lds_tr<D>(smem, ad.tr(0, dt) + KO + u * RB, ad.tr(1, dt) + KO + u * RB);
+    }
     sched_fence();
     const int d0 = key0 - pos;   // distance of this wave's first key
     bool near = false;
@@ -181,23 +199,46 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, A
       for (int r = 0; r < 16; ++r)
         if (c_row(r, g) >= first) sT[r] = 0.0f;
     }
+    float ds = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dpT[r] = sT[r] * dpT[r];
+    for (int r = 0; r < 16; ++r) {
+      dpT[r] = sT[r] * dpT[r];
+      ds += dpT[r];
+    }
+    drow += ds;
+    if constexpr (!MAIN) return;
     if constexpr (BIAS) {
       if (near) {
+        float da = 0.0f, db = 0.0f;   // diagonals ln and ln - 32
+        const int eg = ln - 8 * g;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int x = d0 + c_row(r, g);
-          sumL += x <= -far ? dpT[r] : 0.0f;
-          sumR += x >= far ? dpT[r] : 0.0f;
-          if (x > -far && x < far) atomicAdd(mine + x + far, dpT[r]);
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+          for (int r = 0; r < 8; ++r) skew[32 * (c_row(8 * u + r, g) - 16 * u) + ln] = dpT[8 * u + r];
+          asm volatile("" ::: "memory");
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {   // key 16 u + 8 g + k
+            const float v = skew[32 * (8 * g + k) + ((16 * u + k - eg) & 31)];
+            da += eg <= 16 * u + k ? v : 0.0f;
+            db += eg <= 16 * u + k ? 0.0f : v;
+          }
+          asm volatile("" ::: "memory");
         }
+        da = half_sum(da);
+        db = half_sum(db);
+        const int d = key0 - (s.pos + q0 + 32 * wave_uniform(qh)) + ln - 32 * g;
+        const float v = g ? db : da;
+        if (d <= -far) sumL += v;
+        else if (d >= far) sumR += v;
+        else dist[w * width + d + far] = v;
       } else {
-        float x = 0.0f;
+        float ps = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x += dpT[r];
-        sumL += d0 < 0 ? x : 0.0f;
-        sumR += d0 < 0 ? 0.0f : x;
+        for (int r = 0; r < 16; ++r) ps += sT[r];
+        sumL += d0 < 0 ? ds : 0.0f;
+        sumR += d0 < 0 ? 0.0f : ds;
+        pL += d0 < 0 ? ps : 0.0f;
+        pR += d0 < 0 ? 0.0f : ps;
       }
     }
 #pragma unroll
@@ -207,11 +248,36 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dq_kernel(Attn a, A
       for (int dt = 0; dt < NT; ++dt) dqT[dt] = mfma32(ta[u][dt], sb, dqT[dt]);   // K_j^T dS^T
     }
   };
-  for (int j = 0; j < steps; j += 2) {
-    step(j, 0);
-    if (j + 1 < steps) step(j + 1, 1);
+  // the two key halves' sums of a query
+  auto both = [&](float x) {
+    x = half_sum(x);
+    __syncthreads();
+    if (g == 0) stat[kh * kBlk + qh * 32 + ln] = x;
+    __syncthreads();
+    return stat[qh * 32 + ln] + stat[kBlk + qh * 32 + ln];
+  };
+  const std::integral_constant<bool, true> main;
+  if (steps <= 2 && steps > 0) {
+    const std::integral_constant<bool, false> probe;
+    nDq = 0.0f;
+    step(probe, 0, 0);
+    if (steps > 1) step(probe, 1, 1);
+    dsum = both(drow);
+    nDq = -dsum;
+    drow = 0.0f;
+    issue(0, 0);
   }
-  if constexpr (BIAS) table_part<8>(a, dist, width, sumL, sumR, tpart + ((size_t)bh * tiles + i) * bucket_count(a.bias));
+  for (int j = 0; j < steps; j += 2) {
+    step(main, j, 0);
+    if (j + 1 < steps) step(main, j + 1, 1);
+  }
+  {
+    const float dd = both(drow);
+    if (kh == 0 && g == 0 && live) Ds[li] = dsum + dd;
+    sumL -= dd * pL;
+    sumR -= dd * pR;
+  }
+  if constexpr (BIAS) table_part<4>(a, dist, width, sumL, sumR, tpart + ((size_t)bh * tiles + i) * bucket_count(a.bias));
   // ---- add the two key halves in a row-major staging area, then every thread stores 8-byte pieces of whole rows
   __syncthreads();   // every wave is done with the tiles
   constexpr int C4 = D / 4, NIT = kBlk * C4 / 256, SP = Lds::SP;
@@ -578,7 +644,7 @@ template <int D>
 hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
   const BwdPlan p = attn_bwd_plan(a, ws);
   {
-    const int lds = DqLds<D>::FIXED + (a.has_bias() ? dq_bias_lds(a.bias.far) : 0);
+    const int lds = dq_lds<D>(a);
     auto kern = a.has_bias() ? attn_dq_kernel<D, true> : attn_dq_kernel<D, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dq", st);
