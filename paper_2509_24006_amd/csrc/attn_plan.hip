@@ -39,10 +39,11 @@ AttnPlan attn_plan(const Attn& a, char* ws) {
   p.own = part_of(a.B * a.H / heads, heads, (long long)heads * a.Nq, packed);
   const long long T = ceil_div(a.Nk, kBlk), Tp = ceil_div(a.Np, kBlk);
   if (a.Np > 0) p.prefix = part_of(a.H / heads, heads, (long long)a.B * heads * a.Nq, true);
-  // Parts of about equal length that fill the chip once, two key tiles or more each (less does not pay for a part's
-  // fixed cost and its sums).
+  // Parts of about equal length, two key tiles or more each (less does not pay for a part's fixed cost and its sums),
+  // as many as run at a time: one more would wait for a whole round.
   const long long tiles = (long long)p.own.units * p.own.tiles, ptiles = (long long)p.prefix.units * p.prefix.tiles;
-  const long long len = std::max(2ll, ceil_div(tiles * T + ptiles * Tp, kSlots));
+  long long len = std::max(2ll, ceil_div(tiles * T + ptiles * Tp, kSlots));
+  while (tiles * ceil_div(T, len) + ptiles * ceil_div(Tp, len) > kSlots && len < std::max(T, Tp)) ++len;
   p.own.splits = (int)std::max(1ll, std::min(ceil_div(T, len), 256ll));
   p.prefix.splits = (int)std::max(1ll, std::min(ceil_div(Tp, len), 256ll));
   p.parts = a.Np > 0 || p.own.splits > 1;
@@ -90,13 +91,16 @@ __device__ __forceinline__ void put_pair(bf16* p, float x, float y) {
 __device__ __forceinline__ void put_one(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put_one(bf16* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }
 
-// O = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i over the parts of a row, a wave per row.  The order is that of the parts.
-template <class E, int D>
+// O = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i over the parts of a row.  W waves share a row (each takes every W-th
+// part, eight loads in flight) and meet in LDS; the order of the sums follows from the number of parts.  Bound by the
+// latency of its two rounds of loads.
+template <class E, int D, int W>
 __global__ __launch_bounds__(256) void attn_join_kernel(Attn a, AttnPlan plan) {
-  const int l = threadIdx.x & 63;
-  const long long row = (long long)blockIdx.x * 4 + wave_uniform(threadIdx.x >> 6);
-  if (row >= (long long)a.B * a.H * a.Nq) return;
-  const int n = row % a.Nq, bh = row / a.Nq, b = bh / a.H, h = bh - b * a.H;
+  __shared__ float red[W > 1 ? 4 : 1][D];
+  const int l = threadIdx.x & 63, w = wave_uniform(threadIdx.x >> 6), sub = w % W;
+  const long long row = (long long)blockIdx.x * (4 / W) + w / W;
+  const bool in = row < (long long)a.B * a.H * a.Nq;
+  const int n = in ? row % a.Nq : 0, bh = in ? row / a.Nq : 0, b = bh / a.H, h = bh - b * a.H;
   const AttnPart &ow = plan.own, &pp = plan.prefix;
   const int u = h / ow.heads, hg = h - u * ow.heads;
   // first slot and row of this query among the prefix's and its own sums
@@ -105,7 +109,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a, AttnPlan plan) {
   const size_t os = ow.slot0 + ((size_t)(b * (a.H / ow.heads) + u) * ow.tiles + orow / kBlk) * ow.splits;
   const int np = pp.blocks ? pp.splits : 0, total = np + ow.splits;
   auto at = [&](int i) { return i < np ? (ps + i) * kBlk + pr % kBlk : (os + i - np) * kBlk + orow % kBlk; };
-  // statistics: part i in lane i, i + 64, ...
+  // statistics: part i in lane i % 64
   float M = -INFINITY;
   for (int i = l; i < total; i += 64) {
     const float2 x = *reinterpret_cast<const float2*>(plan.stat + 2 * at(i));
@@ -123,15 +127,32 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a, AttnPlan plan) {
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
     lsum += s;
     const int cnt = min(64, total - i0);
-#pragma unroll 4
-    for (int i = 0; i < cnt; ++i) {
-      const float wi = __shfl(wt, i);
-      if (wi == 0.0f) continue;   // (sums of a part without a key are not written)
-      const float* p = plan.part + at(i0 + i) * D + (D / 64) * l;
+    for (int i = sub; i < cnt; i += 8 * W) {
+      float y[8][D / 64], wi[8];
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(wi, p[e], acc[e]);
+      for (int k = 0; k < 8; ++k) {   // (past the end, and parts without a key, whose sums are not written: nothing is read)
+        wi[k] = i + k * W < cnt ? __shfl(wt, (i + k * W) & 63) : 0.0f;
+        const float* p = plan.part + at(i0 + min(i + k * W, cnt - 1)) * D + (D / 64) * l;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) y[k][e] = wi[k] != 0.0f ? p[e] : 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(wi[k], y[k][e], acc[e]);
     }
   }
+  if constexpr (W > 1) {
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) red[w][(D / 64) * l + e] = acc[e];
+    __syncthreads();
+    if (sub) return;
+#pragma unroll
+    for (int x = 1; x < W; ++x)
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) acc[e] += red[w + x][(D / 64) * l + e];
+  }
+  if (!in) return;
   const float inv = lsum > 0.0f ? 1.0f / lsum : 0.0f;
   E* o = reinterpret_cast<E*>(a.O.p) + b * a.O.sb + h * a.O.sh + (long long)n * a.O.sn + (D / 64) * l;
   if constexpr (D == 128) put_pair(o, acc[0] * inv, acc[1] * inv);
@@ -139,15 +160,22 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a, AttnPlan plan) {
   if (a.L && l == 0) a.L[row] = lsum > 0.0f ? M * kLn2 + logf(lsum) : -INFINITY;
 }
 
+template <class E, int D>
+hipError_t join_impl(const Attn& a, const AttnPlan& plan, hipStream_t st) {
+  const long long rows = (long long)a.B * a.H * a.Nq;
+  const int parts = plan.own.splits + (plan.prefix.blocks ? plan.prefix.splits : 0);
+  KernelTimer kt("attn_join", st);
+  // four waves a row where a wave alone would take a third round of loads
+  if (parts > 8) attn_join_kernel<E, D, 4><<<(unsigned)rows, 256, 0, st>>>(a, plan);
+  else attn_join_kernel<E, D, 1><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, plan);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t attn_join(const Attn& a, const AttnPlan& plan, hipStream_t st) {
-  const unsigned grid = (unsigned)(((long long)a.B * a.H * a.Nq + 3) / 4);
-  auto kern = a.dtype == SLA_F32 ? (a.d == 64 ? attn_join_kernel<float, 64> : attn_join_kernel<float, 128>)
-                                 : (a.d == 64 ? attn_join_kernel<bf16, 64> : attn_join_kernel<bf16, 128>);
-  KernelTimer kt("attn_join", st);
-  kern<<<grid, 256, 0, st>>>(a, plan);
-  return hipGetLastError();
+  if (a.dtype == SLA_F32) return a.d == 64 ? join_impl<float, 64>(a, plan, st) : join_impl<float, 128>(a, plan, st);
+  return a.d == 64 ? join_impl<bf16, 64>(a, plan, st) : join_impl<bf16, 128>(a, plan, st);
 }
 
 // Key tiles alone may not fill the chip (text of a few hundred tokens under a long video), and under a causal mask the
