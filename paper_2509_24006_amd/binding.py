@@ -457,14 +457,6 @@ def sla_attn_forward(p: sla_attn_params, Q, K, V, table=None, q_len=None, k_len=
     """Returns (O, L); L float32 [B,H,Nq] is None when need_L is False.  Q [B,H,Nq,d], K, V [B,Hkv,Nk,d], prefix = (K, V)
     [Hkv,Np,d], or with token_major [B,Nq,H,d], [B,Nk,Hkv,d], [Np,Hkv,d]: views with contiguous features.  Runs on the
     current stream of Q's device."""
-    Kp, Vp = (None, None) if prefix is None else prefix
-    token_major = bool(token_major)
-    r = _host_calls().attn_forward(ctypes.addressof(p), Q, K, V, Kp, Vp, table, q_len, k_len, token_major, O, L, workspace,
-                                   bool(need_L))
-    if type(r) is tuple:
-        return r
-    if r is not None:
-        _check(r, "sla_attn_forward")
     need = sla_attn_sizes(p)[0]
     q = _rows(Q, p, p.H, p.Nq, token_major, "Q")
     k, v = (_rows(t, p, p.Hkv, p.Nk, token_major, n, Q) for n, t in (("K", K), ("V", V)))
@@ -491,13 +483,6 @@ def sla_attn_forward(p: sla_attn_params, Q, K, V, table=None, q_len=None, k_len=
 def sla_attn_backward(p: sla_attn_params, Q, K, V, O, dO, L, table=None, q_len=None, k_len=None, token_major: bool = False,
                       workspace: Optional[torch.Tensor] = None, out=None):
     """Returns (dQ, dK, dV, dtable); dtable, in the table's type, is None without a bias.  out: tensors for the four."""
-    token_major = bool(token_major)
-    r = _host_calls().attn_backward(ctypes.addressof(p), Q, K, V, O, dO, L, table, q_len, k_len, token_major, workspace,
-                                    *((None,) * 4 if out is None else out))
-    if type(r) is tuple:
-        return r
-    if r is not None:
-        _check(r, "sla_attn_backward")
     if p.Np:
         raise SLAError("prefix: there is no backward pass behind one")
     need = sla_attn_sizes(p)[1]

@@ -9,7 +9,12 @@
 // binding.py goes through its own checks and raises what it always raised.  An error code of the
 // library comes back as an integer.  Nothing is kept between calls.
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <cmath>
+#include <cstring>
 
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
@@ -272,12 +277,12 @@ struct AttnCall {
   bool token;   // [B, N, H, d] tensors
   at::Device dev = at::kCPU;
 
-  bool open(PyObject* addr, PyObject* token_major, const at::Tensor* Q) {
-    p = static_cast<const sla_attn_params*>(PyLong_AsVoidPtr(addr));
+  bool open(const sla_attn_params* params, bool token_major, const at::Tensor* Q) {
+    p = params;
     if (!p || !Q || !Q->is_cuda() || sla_attn_sizes(p, &fwd, &bwd) != SLA_OK) return false;
     dt = p->dtype == SLA_F32 ? at::kFloat : at::kBFloat16;
     tt = p->table_dtype == SLA_F32 ? at::kFloat : at::kBFloat16;
-    token = token_major == Py_True;
+    token = token_major;
     dev = Q->device();
     return true;
   }
@@ -302,18 +307,16 @@ struct AttnCall {
     return here(t, type) && t->sizes() == shape && t->is_contiguous();
   }
   // lengths [B] and the table: absent (None) or as stated
-  bool lengths(PyObject* o, const int32_t** out) const {
+  bool lengths(const at::Tensor* t, const int32_t** out) const {
     *out = nullptr;
-    if (o == Py_None) return true;
-    const at::Tensor* t = plain(o);
+    if (!t) return true;
     if (!flat(t, {p->B}, at::kInt)) return false;
     *out = t->const_data_ptr<int32_t>();
     return true;
   }
-  bool table(PyObject* o, const void** out) const {
+  bool table(const at::Tensor* t, const void** out) const {
     *out = nullptr;
-    if (o == Py_None) return p->buckets.n_buckets == 0;
-    const at::Tensor* t = plain(o);
+    if (!t) return p->buckets.n_buckets == 0;
     if (!flat(t, {p->buckets.n_buckets, p->H}, tt)) return false;
     *out = t->const_data_ptr();
     return true;
@@ -327,83 +330,189 @@ struct AttnCall {
   }
 };
 
-// attn_forward(params address, Q, K, V, prefix K, prefix V, table, q_len, k_len, token_major, O, L, workspace, need_L)
-// -> (O, L or None)
-PyObject* attn_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  HANDLE_TH_ERRORS
-  AttnCall c;
-  if (n != 14) Py_RETURN_NONE;
-  const at::Tensor *Q = plain(a[1]), *K = plain(a[2]), *V = plain(a[3]);
-  sla_tensor q, k, v, kp, vp, o;
-  const void* table;
-  const int32_t *q_len, *k_len;
-  Slot O(a[10]), L(a[11]), ws(a[12]);
-  if (!c.open(a[0], a[9], Q)) Py_RETURN_NONE;
-  const sla_attn_params& p = *c.p;
-  if (!c.rows(Q, p.H, p.Nq, &q) || !c.rows(K, p.Hkv, p.Nk, &k) || !c.rows(V, p.Hkv, p.Nk, &v) || !c.table(a[6], &table) ||
-      !c.lengths(a[7], &q_len) || !c.lengths(a[8], &k_len) || !O.ok([&](auto t) { return c.rows(t, p.H, p.Nq, &o); }) ||
-      !L.ok([&](auto t) { return c.flat(t, {p.B, p.H, p.Nq}, at::kFloat); }) ||
-      !ws.ok([&](auto t) { return t->device() == c.dev && bytes(t, c.fwd); }))
-    Py_RETURN_NONE;
-  if (p.Np ? !c.prefix(plain(a[4]), &kp) || !c.prefix(plain(a[5]), &vp) : a[4] != Py_None || a[5] != Py_None) Py_RETURN_NONE;
-  const bool need = a[13] == Py_True || a[11] != Py_None;
-  void* st;
-  if (!stream_of(*Q, &st)) return nullptr;
-  int rc;
-  {
-    NoGil free;
-    const c10::DeviceGuard guard(c.dev);
-    O.fill([&] { return c.fresh(*Q, p.H, p.Nq, &o); });
-    if (need) L.fill([&] { return at::empty({p.B, p.H, p.Nq}, Q->options().dtype(at::kFloat).requires_grad(false)); });
-    if (c.fwd) ws.fill([&] { return new_bytes(c.fwd, *Q); });
-    rc = sla_attn_forward(c.p, &q, &k, &v, p.Np ? &kp : nullptr, p.Np ? &vp : nullptr, table, q_len, k_len, &o,
-                          need ? (float*)L.ptr() : nullptr, c.fwd ? ws.ptr() : nullptr, c.fwd ? ws.size() : 0, st);
-  }
-  if (rc != SLA_OK) return PyLong_FromLong(rc);
-  if (!need) Py_INCREF(Py_None);
-  return pack({O.object(), need ? L.object() : Py_None});
-  END_HANDLE_TH_ERRORS
+// The whole of dense_attention and cached_attention for plain tensors: parameters, checks, forward call and, where a
+// gradient is wanted, the node of the graph, in one call from Python and none in the backward pass.
+struct Attend {   // what a call is given beside its tensors
+  const sla_buckets* buckets;
+  bool causal, token, cached;
+  double scale;   // 0: 1 / sqrt(d)
+};
+
+const at::Tensor* defined(const at::Tensor& t) { return t.defined() ? &t : nullptr; }
+
+bool attend_params(const Attend& a, const at::Tensor& Q, const at::Tensor& K, const at::Tensor* Kp, const at::Tensor* table,
+                   sla_attn_params* p) {
+  if (Q.dim() != 4 || K.dim() != 4 || (table != nullptr) != (a.buckets != nullptr) || (Kp && Kp->dim() != 3)) return false;
+  const int hx = a.token ? 2 : 1, nx = a.token ? 1 : 2;
+  const auto q = Q.sizes(), k = K.sizes();
+  for (int64_t x : {q[0], q[1], q[2], q[3], k[1], k[2]})
+    if (x > 0x7fffffff) return false;
+  auto code = [](at::ScalarType t) { return t == at::kFloat ? (int)SLA_F32 : t == at::kBFloat16 ? (int)SLA_BF16 : -1; };
+  memset(p, 0, sizeof(*p));
+  p->B = (int)q[0];
+  p->H = (int)q[hx];
+  p->Hkv = (int)k[hx];
+  p->Nq = (int)q[nx];
+  p->Nk = (int)k[nx];
+  p->Np = Kp ? (int)Kp->size(a.token ? 0 : 1) : 0;
+  p->d = (int)q[3];
+  p->dtype = code(Q.scalar_type());
+  p->causal = a.causal;
+  p->q_pos = a.cached ? -p->Nq : p->Nk - p->Nq;
+  p->q_from_end = a.cached;
+  p->table_dtype = table ? code(table->scalar_type()) : (int)SLA_F32;
+  p->scale = (float)(a.scale != 0.0 ? a.scale : 1.0 / std::sqrt((double)p->d));
+  if (a.buckets) p->buckets = *a.buckets;
+  return true;
 }
 
-// attn_backward(params address, Q, K, V, O, dO, L, table, q_len, k_len, token_major, workspace, dQ, dK, dV, dtable)
-// -> (dQ, dK, dV, dtable or None)
-PyObject* attn_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  HANDLE_TH_ERRORS
+// the forward call; false where anything does not fit
+bool attend_forward(const sla_attn_params& p, bool token, const at::Tensor& Q, const at::Tensor& K, const at::Tensor& V,
+                    const at::Tensor* Kp, const at::Tensor* Vp, const at::Tensor* table, const at::Tensor* q_len,
+                    const at::Tensor* k_len, void* st, at::Tensor* O, at::Tensor* L) {
   AttnCall c;
-  if (n != 16) Py_RETURN_NONE;
-  const at::Tensor *Q = plain(a[1]), *K = plain(a[2]), *V = plain(a[3]), *O = plain(a[4]), *dO = plain(a[5]), *L = plain(a[6]);
-  sla_tensor q, k, v, o, go, gq, gk, gv;
-  const void* table;
-  const int32_t *q_len, *k_len;
-  Slot ws(a[11]), dQ(a[12]), dK(a[13]), dV(a[14]), dT(a[15]);
-  if (!c.open(a[0], a[10], Q)) Py_RETURN_NONE;
-  const sla_attn_params& p = *c.p;
-  if (p.Np || !c.rows(Q, p.H, p.Nq, &q) || !c.rows(K, p.Hkv, p.Nk, &k) || !c.rows(V, p.Hkv, p.Nk, &v) ||
-      !c.rows(O, p.H, p.Nq, &o) || !c.rows(dO, p.H, p.Nq, &go) || !c.flat(L, {p.B, p.H, p.Nq}, at::kFloat) ||
-      !c.table(a[7], &table) || !c.lengths(a[8], &q_len) || !c.lengths(a[9], &k_len) ||
-      !dQ.ok([&](auto t) { return c.rows(t, p.H, p.Nq, &gq); }) || !dK.ok([&](auto t) { return c.rows(t, p.Hkv, p.Nk, &gk); }) ||
-      !dV.ok([&](auto t) { return c.rows(t, p.Hkv, p.Nk, &gv); }) || (!table && a[15] != Py_None) ||
-      !dT.ok([&](auto t) { return c.flat(t, {p.buckets.n_buckets, p.H}, c.tt); }) ||
-      !ws.ok([&](auto t) { return t->device() == c.dev && bytes(t, c.bwd); }))
-    Py_RETURN_NONE;
-  void* st;
-  if (!stream_of(*Q, &st)) return nullptr;
-  int rc;
-  {
-    NoGil free;
-    const c10::DeviceGuard guard(c.dev);
-    dQ.fill([&] { return c.fresh(*Q, p.H, p.Nq, &gq); });
-    dK.fill([&] { return c.fresh(*Q, p.Hkv, p.Nk, &gk); });
-    dV.fill([&] { return c.fresh(*Q, p.Hkv, p.Nk, &gv); });
-    if (table)
-      dT.fill([&] { return at::empty({p.buckets.n_buckets, p.H}, Q->options().dtype(c.tt).requires_grad(false)); });
-    ws.fill([&] { return new_bytes(c.bwd, *Q); });
-    rc = sla_attn_backward(c.p, &q, &k, &v, &o, &go, L->const_data_ptr<float>(), table, q_len, k_len, &gq, &gk, &gv,
-                           table ? dT.ptr() : nullptr, ws.ptr(), ws.size(), st);
+  sla_tensor q, k, v, kp, vp, o;
+  const void* tb;
+  const int32_t *ql, *kl;
+  if (!c.open(&p, token, &Q) || !c.rows(&Q, p.H, p.Nq, &q) || !c.rows(&K, p.Hkv, p.Nk, &k) || !c.rows(&V, p.Hkv, p.Nk, &v) ||
+      !c.table(table, &tb) || !c.lengths(q_len, &ql) || !c.lengths(k_len, &kl))
+    return false;
+  if (p.Np && (!c.prefix(Kp, &kp) || !c.prefix(Vp, &vp))) return false;
+  const c10::DeviceGuard guard(c.dev);
+  *O = c.fresh(Q, p.H, p.Nq, &o);
+  if (L) *L = at::empty({p.B, p.H, p.Nq}, Q.options().dtype(at::kFloat).requires_grad(false));
+  at::Tensor ws;
+  if (c.fwd) ws = new_bytes(c.fwd, Q);
+  return sla_attn_forward(&p, &q, &k, &v, p.Np ? &kp : nullptr, p.Np ? &vp : nullptr, tb, ql, kl, &o,
+                          L ? L->data_ptr<float>() : nullptr, c.fwd ? ws.data_ptr() : nullptr, c.fwd, st) == SLA_OK;
+}
+
+struct DenseAttention : torch::autograd::Function<DenseAttention> {
+  static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& Q, const at::Tensor& K,
+                                                const at::Tensor& V, const std::optional<at::Tensor>& table,
+                                                const at::Tensor* q_len, const at::Tensor* k_len, const sla_attn_params* p,
+                                                bool token, void* st) {
+    at::Tensor O, L;
+    const at::Tensor none, &tb = table ? *table : none;
+    TORCH_CHECK(attend_forward(*p, token, Q, K, V, nullptr, nullptr, defined(tb), q_len, k_len, st, &O, &L), "sla_attn_forward failed");
+    ctx->save_for_backward({Q, K, V, tb, O, L, q_len ? *q_len : none, k_len ? *k_len : none});
+    ctx->saved_data["p"] = std::string(reinterpret_cast<const char*>(p), sizeof(*p));
+    ctx->saved_data["token"] = token;
+    return {O};
   }
-  if (rc != SLA_OK) return PyLong_FromLong(rc);
-  if (!table) Py_INCREF(Py_None);
-  return pack({dQ.object(), dK.object(), dV.object(), table ? dT.object() : Py_None});
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+    const auto s = ctx->get_saved_variables();
+    const at::Tensor &Q = s[0], &K = s[1], &V = s[2], &table = s[3], &O = s[4], &L = s[5];
+    sla_attn_params p;
+    const std::string bytes = ctx->saved_data["p"].toStringRef();
+    memcpy(&p, bytes.data(), sizeof(p));
+    at::Tensor dO = grads[0], dQ, dK, dV, dT;
+    {
+      const at::NoGradGuard none;
+      AttnCall c;
+      const bool opened = c.open(&p, ctx->saved_data["token"].toBool(), &Q);
+      sla_tensor q, k, v, o, go, gq, gk, gv;
+      const void* tb;
+      const int32_t *ql, *kl;
+      auto whole = [](const sla_tensor& t, int64_t esz) {   // (what the library's own check of dO would refuse)
+        return (reinterpret_cast<uintptr_t>(t.data) | (t.stride_b * esz) | (t.stride_h * esz) | (t.stride_n * esz)) % 16 == 0 &&
+               t.stride_n * esz <= 1 << 24;
+      };
+      const int64_t esz = dO.element_size();
+      if (!c.rows(&dO, p.H, p.Nq, &go) || !whole(go, esz) || go.stride_n < p.d) {
+        dO = dO.contiguous();
+        TORCH_CHECK(c.rows(&dO, p.H, p.Nq, &go), "dense_attention: the output's gradient has another type or shape");
+      }
+      TORCH_CHECK(opened && c.rows(&Q, p.H, p.Nq, &q) && c.rows(&K, p.Hkv, p.Nk, &k) && c.rows(&V, p.Hkv, p.Nk, &v) &&
+                      c.rows(&O, p.H, p.Nq, &o) && c.flat(&L, {p.B, p.H, p.Nq}, at::kFloat) && c.table(defined(table), &tb) &&
+                      c.lengths(defined(s[6]), &ql) && c.lengths(defined(s[7]), &kl),
+                  "dense_attention: the saved tensors have changed");
+      const PyGILState_STATE gil = PyGILState_Ensure();
+      void* st = nullptr;
+      const bool have = stream_of(Q, &st);
+      if (!have) PyErr_Clear();
+      PyGILState_Release(gil);
+      TORCH_CHECK(have, "no current stream");
+      const c10::DeviceGuard guard(c.dev);
+      dQ = c.fresh(Q, p.H, p.Nq, &gq);
+      dK = c.fresh(Q, p.Hkv, p.Nk, &gk);
+      dV = c.fresh(Q, p.Hkv, p.Nk, &gv);
+      if (tb) dT = at::empty({p.buckets.n_buckets, p.H}, Q.options().dtype(c.tt).requires_grad(false));
+      const at::Tensor ws = new_bytes(c.bwd, Q);
+      const int rc = sla_attn_backward(&p, &q, &k, &v, &o, &go, L.data_ptr<float>(), tb, ql, kl, &gq, &gk, &gv,
+                                       tb ? dT.data_ptr() : nullptr, ws.data_ptr(), (size_t)ws.numel(), st);
+      TORCH_CHECK(rc == SLA_OK, "sla_attn_backward failed: ", sla_strerror(rc), " (code ", rc, ")");
+    }
+    if (c10::GradMode::is_enabled()) {   // a graph of the gradients: differentiating them raises
+      torch::autograd::variable_list in;
+      for (at::Tensor* t : {&dQ, &dK, &dV, &dT})
+        if (t->defined()) in.push_back(t->requires_grad_(true));
+      const auto out = (*std::make_shared<torch::autograd::DelayedError>(
+          "dense_attention: its gradients cannot be differentiated", (int64_t)in.size()))(std::move(in));
+      dQ = out[0], dK = out[1], dV = out[2];
+      if (out.size() > 3) dT = out[3];
+    }
+    const at::Tensor no;
+    return {dQ, dK, dV, dT, no, no, no, no, no};
+  }
+};
+
+// attend(Q, K, V, prefix K, prefix V, table, q_len, k_len, address of the buckets or 0, causal, scale or None, token_major,
+//        cached) -> O, or None where the Python code has to lay out, check or refuse
+PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 13) Py_RETURN_NONE;
+  const at::Tensor* t[8];
+  for (int i = 0; i < 8; ++i) {
+    t[i] = a[i] == Py_None ? nullptr : plain(a[i]);
+    if (!t[i] && (a[i] != Py_None || i < 3)) Py_RETURN_NONE;
+  }
+  const at::Tensor &Q = *t[0], &K = *t[1], &V = *t[2];
+  if (!Q.is_cuda() || (t[3] != nullptr) != (t[4] != nullptr)) Py_RETURN_NONE;
+  Attend at_;
+  at_.buckets = static_cast<const sla_buckets*>(PyLong_AsVoidPtr(a[8]));
+  at_.causal = PyObject_IsTrue(a[9]) == 1;
+  at_.scale = a[10] == Py_None ? 0.0 : PyFloat_AsDouble(a[10]);
+  at_.token = PyObject_IsTrue(a[11]) == 1;
+  at_.cached = a[12] == Py_True;
+  if (PyErr_Occurred()) return nullptr;
+  if (a[10] != Py_None && !(at_.scale > 0.0)) Py_RETURN_NONE;
+  sla_attn_params p;
+  if (!attend_params(at_, Q, K, t[3], t[5], &p)) Py_RETURN_NONE;
+  void* st;
+  if (!stream_of(Q, &st)) return nullptr;
+  at::Tensor O;
+  bool grad = false;
+  if (!at_.cached && c10::GradMode::is_enabled())
+    for (int i : {0, 1, 2, 5}) grad = grad || (t[i] && t[i]->requires_grad());
+  if (grad) {
+    // (checked first: the node's own forward call may not fail half way)
+    AttnCall c;
+    sla_tensor x;
+    const void* tb;
+    const int32_t* len;
+    const int64_t q = 16 / Q.element_size();
+    bool ok = c.open(&p, at_.token, &Q) && c.table(t[5], &tb) && c.lengths(t[6], &len) && c.lengths(t[7], &len);
+    for (int i = 0; ok && i < 3; ++i) {
+      const int heads = i ? p.Hkv : p.H, rows = i ? p.Nk : p.Nq;
+      ok = c.rows(t[i], heads, rows, &x) && reinterpret_cast<uintptr_t>(x.data) % 16 == 0 &&
+           (p.B < 2 || x.stride_b % q == 0) && (heads < 2 || x.stride_h % q == 0) &&
+           (rows < 2 || (x.stride_n % q == 0 && x.stride_n >= p.d && x.stride_n * Q.element_size() <= 1 << 24 &&
+                         rows * x.stride_n * Q.element_size() < 1ll << 31));
+    }
+    if (!ok) Py_RETURN_NONE;
+    O = DenseAttention::apply(Q, K, V, t[5] ? std::optional<at::Tensor>(*t[5]) : std::nullopt, t[6], t[7],
+                              static_cast<const sla_attn_params*>(&p), at_.token, st)[0];
+  } else {
+    const at::NoGradGuard no;
+    bool ok;
+    {
+      NoGil free;
+      ok = attend_forward(p, at_.token, Q, K, V, t[3], t[4], t[5], t[6], t[7], st, &O, nullptr);
+    }
+    if (!ok) Py_RETURN_NONE;
+  }
+  return THPVariable_Wrap(O);
   END_HANDLE_TH_ERRORS
 }
 
@@ -412,8 +521,7 @@ PyMethodDef g_methods[] = {
     {"forward", (PyCFunction)(void (*)(void))forward, METH_FASTCALL, nullptr},
     {"mask_forward", (PyCFunction)(void (*)(void))mask_forward, METH_FASTCALL, nullptr},
     {"backward", (PyCFunction)(void (*)(void))backward, METH_FASTCALL, nullptr},
-    {"attn_forward", (PyCFunction)(void (*)(void))attn_forward, METH_FASTCALL, nullptr},
-    {"attn_backward", (PyCFunction)(void (*)(void))attn_backward, METH_FASTCALL, nullptr},
+    {"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_sla_host", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

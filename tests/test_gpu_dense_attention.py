@@ -238,6 +238,46 @@ def test_odd_strides_are_laid_out(dt):
     assert bool(torch.isfinite(Qg.grad).all())
 
 
+def test_gradients_of_odd_strides_subclasses_and_recomputed_layers():
+    """what the compiled call hands back to Python, saved-tensor hooks, and a second derivative, which is refused"""
+    from torch.utils.checkpoint import checkpoint
+
+    class Mine(torch.Tensor):
+        pass
+
+    Q, K, V, dO = tensors(BF, 2, 4, 2, 70, 90, 64)
+    lens, table, bk = ints([90, 33]), torch.randn(8, 4, device="cuda"), sla.position_buckets(8, 20)
+    f = lambda q, k, v, t: attn.dense_attention(q, k, v, k_len=lens, table=t, buckets=bk)
+    new = lambda: [t.clone().requires_grad_(True) for t in (Q, K, V, table)]
+    plain = new()
+    O = f(*plain)
+    want = (O.detach(),) + torch.autograd.grad(O, plain, dO)
+
+    wide = torch.zeros(2, 4, 70, 67, device="cuda", dtype=BF)
+    wide[..., 1:65] = Q
+    odd = [wide[..., 1:65].detach().requires_grad_(True)] + new()[1:]
+    O1 = f(*odd)
+    odd_dO = torch.zeros(2, 4, 64, 70, device="cuda", dtype=BF).transpose(2, 3).copy_(dO)
+    got = (O1.detach(),) + torch.autograd.grad(O1, odd, odd_dO)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+    sub = new()
+    O2 = f(sub[0].as_subclass(Mine), *sub[1:])
+    got = (O2.detach(),) + torch.autograd.grad(O2, sub, dO)
+    assert all(torch.equal(torch.as_tensor(a), b) for a, b in zip(got, want))
+
+    again = new()
+    O3 = checkpoint(f, *again, use_reentrant=False)
+    got = (O3.detach(),) + torch.autograd.grad(O3, again, dO)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+    twice = new()
+    g = torch.autograd.grad(f(*twice), twice, dO, create_graph=True)
+    assert all(torch.equal(a.detach(), b) for a, b in zip(g, want[1:]))
+    with pytest.raises(RuntimeError, match="cannot be differentiated|marked with @once_differentiable"):
+        g[0].sum().backward()
+
+
 def test_results_repeat_bit_for_bit():
     for dt in (F32, BF):
         Q, K, V, dO = tensors(dt, 2, 4, 2, 333, 333, 64)
