@@ -27,8 +27,9 @@ __device__ __forceinline__ KeySteps key_steps(const Attn& a, const Seq& s, int j
 
 struct BwdPlan {
   KeyPlan key;
-  float *Ds, *tpart;   // [B][H][Nq]; parts of the table's gradient, [B][H][qtiles][buckets]
-  int qtiles;
+  int shares;          // float: workgroups per query tile
+  int qparts;          // workgroups of the query side per head
+  float *Ds, *tpart;   // [B][H][Nq]; parts of the table's gradient, [B][H][qparts][buckets]
   size_t bytes;
 };
 BwdPlan attn_bwd_plan(const Attn& a, char* ws);

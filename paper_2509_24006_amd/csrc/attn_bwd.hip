@@ -358,14 +358,14 @@ __device__ __forceinline__ void store_keys(const Attn& a, const AttnGrads& gr, u
 
 template <int D, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(Attn a, AttnGrads gr, const float* __restrict__ Ds, KeyPlan kp,
-                                                            const float* __restrict__ tpart, int qtiles) {
+                                                            const float* __restrict__ tpart, int qparts) {
   using Lds = DkLds<D>;
   using T = SwzTile<D>;
   constexpr int NT = D / 32, KT = D / 16, HT = NT / 2;
   constexpr int RB = 16 * T::ROW_BYTES;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   if ((int)blockIdx.x >= kp.blocks * kp.pieces) {
-    if constexpr (BIAS) table_sum(a, gr, tpart, qtiles, blockIdx.x - kp.blocks * kp.pieces, smem);
+    if constexpr (BIAS) table_sum(a, gr, tpart, qparts, blockIdx.x - kp.blocks * kp.pieces, smem);
     return;
   }
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 5, ln = l & 31;
@@ -648,7 +648,7 @@ hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_
     auto kern = a.has_bias() ? attn_dq_kernel<D, true> : attn_dq_kernel<D, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dq", st);
-    kern<<<dim3(block_row(p.qtiles), block_rows(a.B * a.H, p.qtiles)), 256, lds, st>>>(a, g, p.Ds, p.tpart, p.qtiles);
+    kern<<<dim3(block_row(p.qparts), block_rows(a.B * a.H, p.qparts)), 256, lds, st>>>(a, g, p.Ds, p.tpart, p.qparts);
   }
   const int tables = g.dtable ? a.H : 0, grid = p.key.blocks * p.key.pieces + tables;
   if (grid == 0) return hipGetLastError();
@@ -657,7 +657,7 @@ hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_
     auto kern = a.has_bias() ? attn_dkdv_kernel<D, true> : attn_dkdv_kernel<D, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dkdv", st);
-    kern<<<grid, 256, lds, st>>>(a, g, p.Ds, p.key, p.tpart, p.qtiles);
+    kern<<<grid, 256, lds, st>>>(a, g, p.Ds, p.key, p.tpart, p.qparts);
   }
   if (p.key.pieces > 1) {
     KernelTimer kt("attn_kv_join", st);

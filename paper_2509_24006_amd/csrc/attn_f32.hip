@@ -122,27 +122,44 @@ __global__ __launch_bounds__(256, 2) void attn_f32_fwd_kernel(Attn a, AttnPlan p
 }
 
 // ------------------------------------------------------------------ dQ
-// As in the forward kernel, lane = query; D = rowsum(dO O).  V_{s+1} lands under the scores and dQ of step s, K_{s+1} under
-// dP of step s + 1.  The table's gradient as in the bf16 path; the four quarters of a wave hold the same queries, so they
-// add to the wave's array one after the other, which keeps the order of the additions fixed.
+// Lane = query; D = rowsum(dO O).  A workgroup owns 64 / QW queries; the QW waves that share 16 of them split the 64 keys of
+// every step, and their sums meet in LDS at the end: parts of a tile fill the chip where there are few tiles.  V_{s+1}
+// lands under the scores and dQ of step s, K_{s+1} under dP of step s + 1.  The table's gradient: see
+// table_part; the four quarters of a wave hold the same queries, so they add to the wave's array one after the other, which
+// keeps the order of the additions fixed.
 template <int D>
 constexpr int f32_dq_lds(int far) { return 2 * FTile<D>::BYTES + 5 * (2 * far + 1) * 4 + 32; }
 
-template <int D, bool BIAS>
+// the sums of the QW waves that share 16 tokens; wave wq gets the feature tiles wq, wq + QW, ...  x: [wave][tile][lane]
+template <int QW, int NT>
+__device__ __forceinline__ void add_shares(f32x4* x, const f32x4 (&part)[NT], int w, int l, f32x4 (&sum)[NT / QW]) {
+#pragma unroll
+  for (int f = 0; f < NT; ++f) x[(w * NT + f) * 64 + l] = part[f];
+  __syncthreads();
+#pragma unroll
+  for (int m = 0; m < NT / QW; ++m) {
+    sum[m] = zero4();
+#pragma unroll
+    for (int q = 0; q < QW; ++q) sum[m] += x[((w / QW * QW + q) * NT + w % QW + QW * m) * 64 + l];
+  }
+}
+
+template <int D, int QW, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attn_f32_dq_kernel(Attn a, AttnGrads gr, float* __restrict__ Ds,
                                                               float* __restrict__ tpart, int tiles) {
-  constexpr int NT = D / 16, TB = FTile<D>::BYTES;
+  constexpr int NT = D / 16, TB = FTile<D>::BYTES, NQ = 4 / QW, NO = NT / QW, ROWS = kBlk / QW;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, w = wave_uniform(tid >> 6), l = tid & 63, g = l >> 4, nl = l & 15;
+  const int wk = w / QW, wq = w % QW;
   const BlockOf own = block_of(blockIdx.y, blockIdx.x, a.B * a.H, tiles);
   if (own.i < 0) return;
   const int bh = wave_uniform(own.bh), i = wave_uniform(a.causal ? tiles - 1 - own.i : own.i);
   const int b = bh / a.H, h = bh - b * a.H, hk = h / a.G;
   const Seq s = seq_of(a, b);
-  const int q0 = i * kBlk, n = q0 + 16 * w + nl, pos = s.pos + n;
+  const int q0 = i * ROWS, n = q0 + 16 * wk + nl, pos = s.pos + n;
   const bool in = n < a.Nq, live = n < s.nq;
   int limmax = q0 < s.nq ? s.nk : 0;
-  if (a.causal) limmax = max(0, min(limmax, s.pos + min(q0 + kBlk, s.nq)));
+  if (a.causal) limmax = max(0, min(limmax, s.pos + min(q0 + ROWS, s.nq)));
   const int steps = wave_uniform((limmax + kBlk - 1) / kBlk);
   const int lim = !live ? 0 : a.causal ? max(0, min(s.nk, pos + 1)) : s.nk;
   FLoader<D> lk, lv;
@@ -164,7 +181,7 @@ __global__ __launch_bounds__(256, 2) void attn_f32_dq_kernel(Attn a, AttnGrads g
     f32x4 of[NT];
     load_frag<NT>(row_ptr(a.O, b, h, nc), live, g, of);
     Dr = dot_frag<NT>(gf, of);
-    if (live && g == 0) Ds[(size_t)bh * a.Nq + n] = Dr;
+    if (live && g == 0 && wq == 0) Ds[(size_t)bh * a.Nq + n] = Dr;
   }
   const float Lr = live ? a.L[(size_t)bh * a.Nq + n] : 0.0f;
   float* const bias = reinterpret_cast<float*>(smem + 2 * TB);
@@ -177,21 +194,23 @@ __global__ __launch_bounds__(256, 2) void attn_f32_dq_kernel(Attn a, AttnGrads g
   float sumL = 0.0f, sumR = 0.0f;
 #pragma unroll
   for (int t = 0; t < NT; ++t) dq[t] = zero4();
+  const unsigned char* const Ks = smem + 16 * NQ * wq * FTile<D>::ROWB;   // this wave's keys
+  const unsigned char* const Vs = Ks + TB;
   wait_vm0();
   __syncthreads();
   for (int j = 0; j < steps; ++j) {
     const bool more = j + 1 < steps;
-    const int key0 = j * kBlk;
-    f32x4 p[4], dp[4];
+    const int key0 = j * kBlk + 16 * NQ * wq;
+    f32x4 p[NQ], dp[NQ];
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt) p[kt] = dp[kt] = zero4();
-    mm_rows<D, 4, NT>(ad, smem + TB, gf, dp);    // dP^T = V dO^T
+    for (int kt = 0; kt < NQ; ++kt) p[kt] = dp[kt] = zero4();
+    mm_rows<D, NQ, NT>(ad, Vs, gf, dp);          // dP^T = V dO^T
     wait_vm0();
     __syncthreads();                             // K_j is there, the V slot is free
     if (more) lv.load(dV, j + 1, TB);
-    mm_rows<D, 4, NT>(ad, smem, qf, p);          // S^T = K Q^T
+    mm_rows<D, NQ, NT>(ad, Ks, qf, p);           // S^T = K Q^T
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
+    for (int kt = 0; kt < NQ; ++kt)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int key = key0 + 16 * kt + 4 * g + r;
@@ -201,9 +220,9 @@ __global__ __launch_bounds__(256, 2) void attn_f32_dq_kernel(Attn a, AttnGrads g
       }
     if constexpr (BIAS) {
       const int d0 = key0 - pos;
-      if (__any(d0 + 63 > -far && d0 < far)) {
+      if (__any(d0 + 16 * NQ - 1 > -far && d0 < far)) {
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+        for (int kt = 0; kt < NQ; ++kt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int d = d0 + 16 * kt + 4 * g + r;
@@ -219,25 +238,25 @@ __global__ __launch_bounds__(256, 2) void attn_f32_dq_kernel(Attn a, AttnGrads g
       } else {
         float t = 0.0f;
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
+        for (int kt = 0; kt < NQ; ++kt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) t += dp[kt][r];
         sumL += d0 < 0 ? t : 0.0f;
         sumR += d0 < 0 ? 0.0f : t;
       }
     }
-    mm_over<D, 4, NT>(ad, smem, dp, dq);         // dQ^T += K^T dS^T
+    mm_over<D, NQ, NT>(ad, Ks, dp, dq);          // dQ^T += K^T dS^T
     wait_vm0();
     __syncthreads();                             // V_{j+1} is there, the K slot is free
     if (more) lk.load(dK, j + 1, 0);
   }
   if constexpr (BIAS) table_part<4>(a, dist, width, sumL, sumR, tpart + ((size_t)bh * tiles + i) * bucket_count(a.bias));
+  f32x4 out[NO];
+  add_shares<QW, NT>(reinterpret_cast<f32x4*>(smem), dq, w, l, out);   // (the tiles are consumed)
   if (!in) return;
+  float* const o = row_ptr(gr.dQ, b, h, n) + 16 * wq + 4 * g;
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) dq[t][r] *= a.scale;
-  store_frag<NT>(row_ptr(gr.dQ, b, h, n), g, dq);
+  for (int m = 0; m < NO; ++m) *reinterpret_cast<f32x4*>(o + 16 * QW * m) = out[m] * a.scale;
 }
 
 // ------------------------------------------------------------------ dK, dV
@@ -249,11 +268,11 @@ constexpr int f32_key_lds() { return 2 * FTile<D>::BYTES + 512; }   // + L, D of
 
 template <int D, int QW, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attn_f32_key_kernel(Attn a, AttnGrads gr, const float* __restrict__ Ds, KeyPlan kp,
-                                                               const float* __restrict__ tpart, int qtiles) {
+                                                               const float* __restrict__ tpart, int qparts) {
   constexpr int NT = D / 16, TB = FTile<D>::BYTES, NQ = 4 / QW, NO = NT / QW;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   if ((int)blockIdx.x >= kp.blocks * kp.pieces) {
-    if constexpr (BIAS) table_sum(a, gr, tpart, qtiles, blockIdx.x - kp.blocks * kp.pieces, smem);
+    if constexpr (BIAS) table_sum(a, gr, tpart, qparts, blockIdx.x - kp.blocks * kp.pieces, smem);
     return;
   }
   const unsigned char* stat = smem + 2 * TB;
@@ -340,29 +359,10 @@ __global__ __launch_bounds__(256, 2) void attn_f32_key_kernel(Attn a, AttnGrads 
       h = hn;
     }
   }
-  // wave wq of the QW that share 16 keys gets the feature tiles wq, wq + QW, ...
   f32x4 ok_[NO], ov[NO];
-  f32x4* x = reinterpret_cast<f32x4*>(smem);      // [wave][dK, dV][tile][lane]
-#pragma unroll
-  for (int f = 0; f < NT; ++f) {
-    x[(2 * w * NT + f) * 64 + l] = dk[f];
-    x[((2 * w + 1) * NT + f) * 64 + l] = dv[f];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int m = 0; m < NO; ++m) {
-    ok_[m] = ov[m] = zero4();
-#pragma unroll
-    for (int q = 0; q < QW; ++q) {
-      const int at = (2 * (wk * QW + q) * NT + wq + QW * m) * 64 + l;
-      const f32x4 c = x[at], d = x[at + NT * 64];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        ok_[m][r] += c[r];
-        ov[m][r] += d[r];
-      }
-    }
-  }
+  f32x4* const x = reinterpret_cast<f32x4*>(smem);
+  add_shares<QW, NT>(x, dk, w, l, ok_);
+  add_shares<QW, NT>(x + 4 * NT * 64, dv, w, l, ov);
   float *oK, *oV;
   if (st.total > kp.piece) {
     oK = kp.part + (((size_t)bh * kp.tiles + j) * kp.pieces + p) * (2 * kBlk * D) + (size_t)(key - j * kBlk) * D;
@@ -433,7 +433,7 @@ hipError_t launch_key(const Attn& a, const AttnGrads& g, const BwdPlan& p, hipSt
     auto kern = a.has_bias() ? attn_f32_key_kernel<D, QW, true> : attn_f32_key_kernel<D, QW, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dkdv", st);
-    kern<<<grid, 256, lds, st>>>(a, g, p.Ds, p.key, p.tpart, p.qtiles);
+    kern<<<grid, 256, lds, st>>>(a, g, p.Ds, p.key, p.tpart, p.qparts);
   }
   if (p.key.pieces > 1) {
     KernelTimer kt("attn_kv_join", st);
@@ -442,16 +442,20 @@ hipError_t launch_key(const Attn& a, const AttnGrads& g, const BwdPlan& p, hipSt
   return hipGetLastError();
 }
 
+template <int D, int QW>
+hipError_t launch_dq(const Attn& a, const AttnGrads& g, const BwdPlan& p, hipStream_t st) {
+  const int lds = a.has_bias() ? f32_dq_lds<D>(a.bias.far) : 2 * FTile<D>::BYTES;
+  auto kern = a.has_bias() ? attn_f32_dq_kernel<D, QW, true> : attn_f32_dq_kernel<D, QW, false>;
+  SLA_TRY(ensure_dyn_lds(kern, lds));
+  KernelTimer kt("attn_dq", st);
+  kern<<<dim3(block_row(p.qparts), block_rows(a.B * a.H, p.qparts)), 256, lds, st>>>(a, g, p.Ds, p.tpart, p.qparts);
+  return hipGetLastError();
+}
+
 template <int D>
 hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_t st) {
   const BwdPlan p = attn_bwd_plan(a, ws);
-  {
-    const int lds = a.has_bias() ? f32_dq_lds<D>(a.bias.far) : 2 * FTile<D>::BYTES;
-    auto kern = a.has_bias() ? attn_f32_dq_kernel<D, true> : attn_f32_dq_kernel<D, false>;
-    SLA_TRY(ensure_dyn_lds(kern, lds));
-    KernelTimer kt("attn_dq", st);
-    kern<<<dim3(block_row(p.qtiles), block_rows(a.B * a.H, p.qtiles)), 256, lds, st>>>(a, g, p.Ds, p.tpart, p.qtiles);
-  }
+  SLA_TRY((p.shares == 4 ? launch_dq<D, 4>(a, g, p, st) : p.shares == 2 ? launch_dq<D, 2>(a, g, p, st) : launch_dq<D, 1>(a, g, p, st)));
   return p.key.quarters == 4 ? launch_key<D, 4>(a, g, p, st) : launch_key<D, 2>(a, g, p, st);
 }
 

@@ -192,13 +192,17 @@ BwdPlan attn_bwd_plan(const Attn& a, char* ws) {
     return x;
   };
   const bool f32 = a.dtype == SLA_F32;
-  p.qtiles = (a.Nq + kBlk - 1) / kBlk;
+  const int qtiles = (a.Nq + kBlk - 1) / kBlk;
+  // float query side: as many parts of a tile as fill the chip's 512 places
+  const long long qunits = (long long)a.B * a.H * qtiles;
+  p.shares = !f32 || qunits > 256 ? 1 : qunits > 128 ? 2 : 4;
+  p.qparts = (a.Nq + kBlk / p.shares - 1) / (kBlk / p.shares);
   KeyPlan& k = p.key;
   k.tiles = (a.Nk + kBlk - 1) / kBlk;
   const long long units = (long long)a.B * a.Hkv * k.tiles;
   k.quarters = f32 ? (units < 384 ? 4 : 2) : 1;
   k.blocks = units == 0 ? 0 : f32 ? (int)units * k.quarters : block_row(k.tiles) * block_rows(a.B * a.Hkv, k.tiles);
-  const double slots = !f32 && a.d == 64 ? 768 : 512, wgs = (double)units * k.quarters, steps = (double)a.G * p.qtiles;
+  const double slots = !f32 && a.d == 64 ? 768 : 512, wgs = (double)units * k.quarters, steps = (double)a.G * qtiles;
   double best = 1e300;
   k.pieces = 1;
   for (int n = 1; n <= 64 && n <= steps; ++n) {
@@ -212,7 +216,7 @@ BwdPlan attn_bwd_plan(const Attn& a, char* ws) {
   }
   k.piece = k.pieces > 1 ? (int)ceil(steps / k.pieces) : 0x7fffffff;
   p.Ds = take((size_t)a.B * a.H * a.Nq);
-  p.tpart = take(a.has_bias() ? (size_t)a.B * a.H * p.qtiles * bucket_count(a.bias) : 0);
+  p.tpart = take(a.has_bias() ? (size_t)a.B * a.H * p.qparts * bucket_count(a.bias) : 0);
   k.part = take(k.pieces > 1 ? (size_t)units * k.pieces * 2 * kBlk * a.d : 0);
   p.bytes = off;
   return p;
