@@ -29,7 +29,8 @@ struct BwdPlan {
   KeyPlan key;
   int shares;          // float: workgroups per query tile
   int qparts;          // workgroups of the query side per head
-  float *Ds, *tpart;   // [B][H][Nq]; parts of the table's gradient, [B][H][qparts][buckets]
+  float* stat;         // what the key side needs of every query: float D, bf16 L and D as an operand (16 bytes)
+  float* tpart;        // parts of the table's gradient, [B][H][qparts][buckets]
   size_t bytes;
 };
 BwdPlan attn_bwd_plan(const Attn& a, char* ws);

@@ -25,6 +25,24 @@ __device__ __forceinline__ void expand_bias(const Attn& a, int h, float* out) {
   for (int i = threadIdx.x; i <= 2 * a.bias.far; i += 256) out[i] = table_at(a, bucket_of(a.bias, i - a.bias.far), h) * kLog2e;
 }
 
+// A query's L / scale and D, each as three bf16 terms (24 bits): the A operand of one more k-step of the key side's first
+// products, whose B operands hold -1 at the places of one or the other, so that the accumulators come out as
+// S - L / scale and dP - D.
+typedef bf16x8 RowStat;
+__device__ __forceinline__ RowStat row_stat(float L, float D, float rscale) {
+  const float l = L == -INFINITY ? 1e30f : L * rscale;   // (a row without a key: P = 0)
+  RowStat r = zero_bf16x8();
+  float x = l, y = D;
+#pragma unroll
+  for (int e = 0; e < 3; ++e) {
+    r[e] = (__bf16)x;
+    r[4 + e] = (__bf16)y;
+    x -= (float)r[e];
+    y -= (float)r[4 + e];
+  }
+  return r;
+}
+
 // ------------------------------------------------------------------ dQ
 template <int D>
 struct DqLds {
@@ -54,8 +72,8 @@ int dq_lds(const Attn& a) { return a.has_bias() ? DqLds<D>::BIAS + 5 * (2 * a.bi
 // distances move on by 64 and span 63), so that the sum is stored, not added: no atomics, which take a cycle per lane.
 // (768 workgroups of up to 8 steps: 64 us with LDS atomics, 32 this way.)
 template <int D, bool BIAS>
-__global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(Attn a, AttnGrads gr, float* __restrict__ Ds,
-                                                                        float* __restrict__ tpart, int tiles) {
+__global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(Attn a, AttnGrads gr, RowStat* __restrict__ stats,
+                                                                                float* __restrict__ tpart, int tiles) {
   using Lds = DqLds<D>;
   using T = SwzTile<D>;
   constexpr int NT = D / 32, KT = D / 16, RB = 16 * T::ROW_BYTES;
@@ -76,11 +94,12 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
   const int lim = !live ? 0x7fffffff : a.causal ? max(0, min(s.nk, pos + 1)) : s.nk;   // (rows that are not live: dO = 0)
   const float sl2 = a.scale * kLog2e;
 
-  TileLoader<D> tq, tg, tk, tv;
+  TileLoader<D> tq, tg;
+  RunLoader<D> tk, tv;
   tq.init(lds_base(smem), w, l, 2 * a.Q.sn);
   tg.init(lds_base(smem), w, l, 2 * gr.dO.sn);
-  tk.init(lds_base(smem), w, l, 2 * a.K.sn);
-  tv.init(lds_base(smem), w, l, 2 * a.V.sn);
+  tk.init(lds_base(smem), w, l, 2 * a.K.sn, kBlk);
+  tv.init(lds_base(smem), w, l, 2 * a.V.sn, kBlk);
   tq.load(rows_rsrc<D>(a.Q, b, h, s.nq), i, Lds::BUF);
   tg.load(rows_rsrc<D>(gr.dO, b, h, s.nq), i, Lds::BUF + Lds::TILE);
   const size_t li = (size_t)bh * a.Nq + n;
@@ -114,11 +133,16 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
     }
   }
   const BufDesc descK = rows_rsrc<D>(a.K, b, hk, s.nk), descV = rows_rsrc<D>(a.V, b, hk, s.nk);
-  auto issue = [&](int j, const int bufi) __attribute__((always_inline)) {
-    tk.load(descK, j, bufi * Lds::BUF);
-    tv.load(descV, j, bufi * Lds::BUF + Lds::TILE);
+  const std::integral_constant<int, 0> b0;   // the two pair buffers
+  const std::integral_constant<int, 1> b1;
+  auto issue = [&](int j, auto Buf) __attribute__((always_inline)) {
+    constexpr int O = decltype(Buf)::value * Lds::BUF;
+    tk.template load<O>(descK, j * tk.tile_step);
+    tv.template load<O + Lds::TILE>(descV, j * tv.tile_step);
   };
-  if (steps > 0) issue(0, 0);
+  if (steps > 0) issue(0, b0);
+  tk.pin();
+  tv.pin();
   float dsum = 0.0f;
 #pragma unroll
   for (int t = 0; t < KT; ++t) {
@@ -137,14 +161,14 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
   TileAddr<D> ad;   // this wave reads rows 32 kh .. of K_j and V_j
   ad.init(32 * kh, l);
   // MAIN: the step proper; else only drow
-  auto step = [&](auto Main, int j, const int buf) __attribute__((always_inline)) {
+  auto step = [&](auto Main, int j, auto Buf) __attribute__((always_inline)) {
     constexpr bool MAIN = decltype(Main)::value;
-    const int KO = buf * Lds::BUF, VO = KO + Lds::TILE;
+    constexpr int buf = decltype(Buf)::value, KO = buf * Lds::BUF, VO = KO + Lds::TILE;
     const int key0 = j * kBlk + 32 * wave_uniform(kh);
     ad.refresh();
     wait_vm0();
     __syncthreads();   // tiles of step j have landed for every wave; step j - 1 is fully consumed
-    if (j + 1 < steps) issue(j + 1, buf ^ 1);
+    if (j + 1 < steps) issue(j + 1, std::integral_constant<int, buf ^ 1>());
     constexpr int PF = 4;   // LDS reads run PF operand pairs ahead of the products
     bf16x8 ka[PF], va[PF], ta[2][NT];
     auto read_s = [&](int t) __attribute__((always_inline)) {
@@ -260,20 +284,20 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
   if (steps <= 2 && steps > 0) {
     const std::integral_constant<bool, false> probe;
     nDq = 0.0f;
-    step(probe, 0, 0);
-    if (steps > 1) step(probe, 1, 1);
+    step(probe, 0, b0);
+    if (steps > 1) step(probe, 1, b1);
     dsum = both(drow);
     nDq = -dsum;
     drow = 0.0f;
-    issue(0, 0);
+    issue(0, b0);
   }
   for (int j = 0; j < steps; j += 2) {
-    step(main, j, 0);
-    if (j + 1 < steps) step(main, j + 1, 1);
+    step(main, j, b0);
+    if (j + 1 < steps) step(main, j + 1, b1);
   }
   {
     const float dd = both(drow);
-    if (kh == 0 && g == 0 && live) Ds[li] = dsum + dd;
+    if (kh == 0 && g == 0 && live) stats[li] = row_stat(a.L[li], dsum + dd, 1.0f / a.scale);
     sumL -= dd * pL;
     sumR -= dd * pR;
   }
@@ -322,8 +346,9 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
 // First products (S, dP): wave (kh, x) takes keys 32 kh .., queries 32 x .. of the pair; S and dP are [query][key], one
 // key per lane.  Second products (dV^T = dO^T P, dK^T = Q^T dS): the same wave takes keys 32 kh .. and the
 // feature half x, over all 64 queries.  P and dS cross between the two waves of a key half through LDS in operand layout.
-// L and D of a query enter the first products as one more k-step: the A operand carries L / scale resp. D split into three
-// bf16 terms (24 bits), the B operand -1, so that the accumulators come out as S - L / scale and dP - D.
+// L and D of a query enter the first products as one more k-step (row_stat).  What counts is the number of instructions
+// (a wave issues one in five cycles or more): loads with one M0 a tile, descriptors that change with the head only, L and
+// D as a ready operand.  (XX)
 template <int D>
 struct DkLds {
   static constexpr int TILE = SwzTile<D>::BYTES;
@@ -357,7 +382,7 @@ __device__ __forceinline__ void store_keys(const Attn& a, const AttnGrads& gr, u
 }
 
 template <int D, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(Attn a, AttnGrads gr, const float* __restrict__ Ds, KeyPlan kp,
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkdv_kernel(Attn a, AttnGrads gr, const RowStat* __restrict__ stats, KeyPlan kp,
                                                             const float* __restrict__ tpart, int qparts) {
   using Lds = DkLds<D>;
   using T = SwzTile<D>;
@@ -390,26 +415,31 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(Attn a, AttnGrads gr,
     dvT[t] = zero_f32x16();
     dkT[t] = zero_f32x16();
   }
-  const float sl2 = a.scale * kLog2e, rscale = 1.0f / a.scale;
+  const float sl2 = a.scale * kLog2e;
   const int wu = wave_uniform(w);
-  TileLoader<D> tq, tg;
-  tq.init(lds_base(smem), w, l, 2 * a.Q.sn);
-  tg.init(lds_base(smem), w, l, 2 * gr.dO.sn);
-  // head and query tile of the step in flight or in use (cur) and of the one after it
-  struct At {
-    int h, i;
-  };
+  RunLoader<D> tq, tg;
+  tq.init(lds_base(smem), w, l, 2 * a.Q.sn, kBlk);
+  tg.init(lds_base(smem), w, l, 2 * gr.dO.sn, kBlk);
+  // head and query tile of the step in flight or in use, and where they lie
   const int i_end = ks_.i0 + ks_.per_head;
-  auto after = [&](At x) __attribute__((always_inline)) { return x.i + 1 < i_end ? At{x.h, x.i + 1} : At{x.h + 1, ks_.i0}; };
-  At cur{hk * a.G, ks_.i0};
+  int ch = hk * a.G, ci = ks_.i0;
   if (cnt > 0) {
     const int hh = s_beg / ks_.per_head;
-    cur = At{wave_uniform(hk * a.G + hh), wave_uniform(ks_.i0 + s_beg - hh * ks_.per_head)};
+    ch = wave_uniform(ch + hh);
+    ci = wave_uniform(ks_.i0 + s_beg - hh * ks_.per_head);
   }
-  auto issue = [&](At x, const int bufi) __attribute__((always_inline)) {
-    const int off = bufi * Lds::BUF;
-    tq.load(rows_rsrc<D>(a.Q, b, x.h, sq.nq), x.i, off);
-    tg.load(rows_rsrc<D>(gr.dO, b, x.h, sq.nq), x.i, off + Lds::TILE);
+  BufDesc descQ, descG, descS;
+  auto turn = [&]() __attribute__((always_inline)) {
+    const int h = min(ch, a.H - 1);   // (behind the last step of the last head: not read)
+    descQ = rows_rsrc<D>(a.Q, b, h, sq.nq);
+    descG = rows_rsrc<D>(gr.dO, b, h, sq.nq);
+    descS = tile_rsrc(stats + ((size_t)b * a.H + h) * a.Nq, sq.nq * 16);
+  };
+  turn();
+  auto issue = [&](auto Buf) __attribute__((always_inline)) {
+    constexpr int O = decltype(Buf)::value * Lds::BUF;
+    tq.template load<O>(descQ, ci * tq.tile_step);
+    tg.template load<O + Lds::TILE>(descG, ci * tg.tile_step);
   };
   {
     TileLoader<D> t;
@@ -418,10 +448,12 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(Attn a, AttnGrads gr,
     t.init(lds_base(smem), w, l, 2 * a.V.sn);
     t.load(rows_rsrc<D>(a.V, b, hk, sq.nk), j, Lds::BUF + Lds::TILE);
   }
-  if (cnt > 0) issue(cur, 0);
+  const std::integral_constant<int, 0> b0;
+  const std::integral_constant<int, 1> b1;
+  if (cnt > 0) issue(b0);
   float* const bias = reinterpret_cast<float*>(smem + Lds::BIAS);
   const int far = a.bias.far;
-  if constexpr (BIAS) expand_bias(a, min(cur.h, a.H - 1), bias);
+  if constexpr (BIAS) expand_bias(a, ch, bias);
   wait_vm0_known();
   __syncthreads();
   {
@@ -442,37 +474,41 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(Attn a, AttnGrads gr,
   ad.init(32 * xh, l);
   TileAddr<D> at;   // second products: transposing reads, feature tiles x HT ..
   at.init(0, l);
-  bf16x8 bneg;      // B operand of the extra k-step: -1 at k = 0, 1, 2
+  bf16x8 bL, bD;    // B operands of the extra k-step
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bneg[e] = (__bf16)((g == 0 && e < 3) ? -1.0f : 0.0f);
+  for (int e = 0; e < 8; ++e) {
+    bL[e] = (__bf16)((g == 0 && e < 3) ? -1.0f : 0.0f);
+    bD[e] = (__bf16)((g == 0 && e >= 4 && e < 7) ? -1.0f : 0.0f);
+  }
+  tq.pin();
+  tg.pin();
   const int xw = Lds::XOFF + ((kh * 4 + 2 * xh) * 2 * 64 + l) * 16;   // this wave's exchange writes
   const int xr = Lds::XOFF + (kh * 4 * 2 * 64 + l) * 16;              // ... and reads
   const int xwave = Lds::XOFF + (kh * 4 + 2 * xh) * 2 * 64 * 16;      // start of this wave's part (uniform)
   const unsigned xstat = lds_base(smem) + wave_uniform(xwave);
-  At next = after(cur);
-  auto step = [&](int s, const int buf) __attribute__((always_inline)) {
-    const int QO = buf * Lds::BUF, GO = QO + Lds::TILE;
+  auto step = [&](int s, auto Buf) __attribute__((always_inline)) {
+    constexpr int buf = decltype(Buf)::value, QO = buf * Lds::BUF, GO = QO + Lds::TILE;
     ad.refresh();
     at.refresh();
     wait_vm0_known();
     __syncthreads();   // tiles of step s have landed for every wave; step s-1 is fully consumed
     // L and D of this step's 64 queries are requested ahead of the next pair's tiles (loads return in order) and picked
-    // up after the first products.  They go global -> LDS into the first 512 bytes of this wave's own part of the exchange
+    // up after the first products.  They go global -> LDS into the first KB of this wave's own part of the exchange
     // area, which it overwrites with P and dS only after it has read them back.  Rows past the end read as 0; their Q
     // and dO rows are zero too, so the finite P they get adds nothing.
-    {
-      const int n0 = cur.i * kBlk, rows = min(kBlk, sq.nq - n0), lo = lane_id() * 4;
-      const size_t li = ((size_t)b * a.H + cur.h) * a.Nq + n0;
-      load_to_lds4(tile_rsrc(a.L + li, rows * 4), lo, xstat);
-      load_to_lds4(tile_rsrc(Ds + li, rows * 4), lo, xstat + 256);
-    }
-    const int qt = cur.i;
+    load_to_lds16(descS, lane_id() * 16, ci * (kBlk * 16), xstat);
+    const int qt = ci;
     // (the last step requests its own pair once more, into the other buffer, where nobody reads it: every step then
     // has the same number of loads in flight and one wait serves all)
-    const At from = s + 1 < s_end ? next : cur;
-    issue(from, buf ^ 1);
-    cur = from;
-    next = after(from);
+    const bool turned = s + 1 < s_end && ci + 1 == i_end;
+    if (turned) {
+      ++ch;
+      ci = ks_.i0;
+      turn();
+    } else if (s + 1 < s_end) {
+      ++ci;
+    }
+    issue(std::integral_constant<int, buf ^ 1>());
     constexpr int PF = 4;   // LDS reads run PF operand pairs ahead of the products
     bf16x8 qa[PF], ga[PF];
     auto read_s = [&](int t) __attribute__((always_inline)) {
@@ -492,24 +528,9 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(Attn a, AttnGrads gr,
     }
     wait_vm<2 * T::IPW>();   // the statistics are there, the tile loads may still fly
     {
-      const int qo = (32 * xh + (lane_id() & 31)) * 4;
-      const float lraw = *reinterpret_cast<const float*>(smem + xwave + qo);
-      const float dcur = *reinterpret_cast<const float*>(smem + xwave + 256 + qo);
-      const float lcur = lraw == -INFINITY ? 1e30f : lraw * rscale;   // (a row without a key: P = 0)
-      bf16x8 aL = zero_bf16x8(), aD = zero_bf16x8();
-      const __bf16 l0 = (__bf16)lcur, d0 = (__bf16)dcur;
-      const float lr = lcur - (float)l0, dr = dcur - (float)d0;
-      const __bf16 l1 = (__bf16)lr, d1 = (__bf16)dr;
-      const __bf16 l2 = (__bf16)(lr - (float)l1), d2 = (__bf16)(dr - (float)d1);
-      const __bf16 z = (__bf16)0.0f;
-      aL[0] = g == 0 ? l0 : z;
-      aL[1] = g == 0 ? l1 : z;
-      aL[2] = g == 0 ? l2 : z;
-      aD[0] = g == 0 ? d0 : z;
-      aD[1] = g == 0 ? d1 : z;
-      aD[2] = g == 0 ? d2 : z;
-      sm = mfma32(aL, bneg, sm);
-      dp = mfma32(aD, bneg, dp);
+      const RowStat st = *reinterpret_cast<const RowStat*>(smem + xwave + (32 * xh + (lane_id() & 31)) * 16);
+      sm = mfma32(st, bL, sm);
+      dp = mfma32(st, bD, dp);
     }
     // operand i of the second products: i = 2 HT ks + 2 dt + which; which 0: dO^T rows of feature tile x HT + dt (for
     // dV), which 1: Q^T (for dK); k = pair rows 16 ks ..
@@ -572,15 +593,15 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(Attn a, AttnGrads gr,
       sched_fence();
     }
     if constexpr (BIAS) {
-      if (cur.i == ks_.i0 && s + 1 < s_end && a.G > 1) {   // the next step is of another head (its bias is read behind the next barrier)
+      if (turned) {   // the next step is of another head (its bias is read behind the next barrier)
         __syncthreads();
-        expand_bias(a, cur.h, bias);
+        expand_bias(a, ch, bias);
       }
     }
   };
   for (int s = s_beg; s < s_end; s += 2) {
-    step(s, 0);
-    if (s + 1 < s_end) step(s + 1, 1);
+    step(s, b0);
+    if (s + 1 < s_end) step(s + 1, b1);
   }
   wait_vm0_known();        // the last step's surplus request has landed
   if (cut) {
@@ -648,7 +669,7 @@ hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_
     auto kern = a.has_bias() ? attn_dq_kernel<D, true> : attn_dq_kernel<D, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dq", st);
-    kern<<<dim3(block_row(p.qparts), block_rows(a.B * a.H, p.qparts)), 256, lds, st>>>(a, g, p.Ds, p.tpart, p.qparts);
+    kern<<<dim3(block_row(p.qparts), block_rows(a.B * a.H, p.qparts)), 256, lds, st>>>(a, g, (RowStat*)p.stat, p.tpart, p.qparts);
   }
   const int tables = g.dtable ? a.H : 0, grid = p.key.blocks * p.key.pieces + tables;
   if (grid == 0) return hipGetLastError();
@@ -657,7 +678,7 @@ hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_
     auto kern = a.has_bias() ? attn_dkdv_kernel<D, true> : attn_dkdv_kernel<D, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dkdv", st);
-    kern<<<grid, 256, lds, st>>>(a, g, p.Ds, p.key, p.tpart, p.qparts);
+    kern<<<grid, 256, lds, st>>>(a, g, (const RowStat*)p.stat, p.key, p.tpart, p.qparts);
   }
   if (p.key.pieces > 1) {
     KernelTimer kt("attn_kv_join", st);

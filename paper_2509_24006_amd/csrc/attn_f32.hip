@@ -433,7 +433,7 @@ hipError_t launch_key(const Attn& a, const AttnGrads& g, const BwdPlan& p, hipSt
     auto kern = a.has_bias() ? attn_f32_key_kernel<D, QW, true> : attn_f32_key_kernel<D, QW, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dkdv", st);
-    kern<<<grid, 256, lds, st>>>(a, g, p.Ds, p.key, p.tpart, p.qparts);
+    kern<<<grid, 256, lds, st>>>(a, g, p.stat, p.key, p.tpart, p.qparts);
   }
   if (p.key.pieces > 1) {
     KernelTimer kt("attn_kv_join", st);
@@ -448,7 +448,7 @@ hipError_t launch_dq(const Attn& a, const AttnGrads& g, const BwdPlan& p, hipStr
   auto kern = a.has_bias() ? attn_f32_dq_kernel<D, QW, true> : attn_f32_dq_kernel<D, QW, false>;
   SLA_TRY(ensure_dyn_lds(kern, lds));
   KernelTimer kt("attn_dq", st);
-  kern<<<dim3(block_row(p.qparts), block_rows(a.B * a.H, p.qparts)), 256, lds, st>>>(a, g, p.Ds, p.tpart, p.qparts);
+  kern<<<dim3(block_row(p.qparts), block_rows(a.B * a.H, p.qparts)), 256, lds, st>>>(a, g, p.stat, p.tpart, p.qparts);
   return hipGetLastError();
 }
 

@@ -215,7 +215,7 @@ BwdPlan attn_bwd_plan(const Attn& a, char* ws) {
     }
   }
   k.piece = k.pieces > 1 ? (int)ceil(steps / k.pieces) : 0x7fffffff;
-  p.Ds = take((size_t)a.B * a.H * a.Nq);
+  p.stat = take((size_t)a.B * a.H * a.Nq * (f32 ? 1 : 4));
   p.tpart = take(a.has_bias() ? (size_t)a.B * a.H * p.qparts * bucket_count(a.bias) : 0);
   k.part = take(k.pieces > 1 ? (size_t)units * k.pieces * 2 * kBlk * a.d : 0);
   p.bytes = off;
