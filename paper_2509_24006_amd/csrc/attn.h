@@ -4,7 +4,7 @@
 #define SLA_ATTN_H_
 
 #include "../../include/sla.h"
-#include "sla_internal.h"
+#include "mfma_common.h"
 
 namespace sla {
 
@@ -62,6 +62,34 @@ __device__ __forceinline__ float table_at(const Attn& a, int bucket, int h) {
   const size_t i = (size_t)bucket * a.H + h;
   return a.table16 ? to_f32(reinterpret_cast<const __hip_bfloat16*>(a.table)[i]) : reinterpret_cast<const float*>(a.table)[i];
 }
+
+// Which head and tile a workgroup of a launch over BH heads of nb tiles owns.  Workgroups are dealt to the 8 XCDs (each with
+// its own L2) round robin, and what a tile reads beside its own rows is read by all tiles of its head and group.  Where
+// the heads can be dealt out evenly, all with the same work, an XCD takes whole heads: one after the other, or under a causal
+// mask, where a tile's work falls with its index, their tiles in turn, the longest first.  Else the XCDs share every head:
+// in ranges (block_of) or, causal, tile by tile across all heads, the longest first.
+// (Forward / query side / key side, us, ranges of every head -> whole heads: 256 heads x 16 tiles, d = 64, 120 / 139 / 195
+// -> 113 / 134 / 187; causal 32 x 64 over 8 K, V heads, d = 128, 193 / 254 / 306 -> 159 / 212 / 300; of two sequences of
+// different lengths, 24 x 512, 239 / 340 / 371 -> 296 / 391 / 415, hence the condition.  Causal 12 x 79 with a bias, d = 64:
+// ranges 103, tile by tile 84.)
+struct TileOf {
+  int bh, i;   // i < 0: a padding workgroup
+};
+struct TileMap {
+  int BH, nb, whole, falling;
+  __device__ __forceinline__ TileOf at(int index) const {
+    if (whole) {
+      const int x = index & 7, m = index >> 3, hp = BH >> 3;
+      return falling ? TileOf{x * hp + m % hp, m / hp} : TileOf{x * hp + m / nb, m % nb};
+    }
+    if (falling) return TileOf{index % BH, index / BH};
+    const int row = block_row(nb), y = index / row;
+    const BlockOf o = block_of(y, index - y * row, BH, nb);
+    return TileOf{o.bh, o.i};
+  }
+  int blocks() const { return nb == 0 ? 0 : whole || falling ? BH * nb : block_row(nb) * block_rows(BH, nb); }
+};
+inline TileMap tile_map(const Attn& a, int BH, int nb) { return TileMap{BH, nb, BH % 8 == 0 && !a.q_len && !a.k_len, a.causal}; }
 
 size_t attn_forward_ws(const Attn& a);
 size_t attn_backward_ws(const Attn& a);

@@ -11,6 +11,7 @@ namespace sla {
 struct KeyPlan {
   int tiles, pieces, piece;   // key tiles; most pieces of one, steps in a piece
   int quarters;               // float: workgroups per key tile
+  TileMap map;                // (bf16)
   int blocks;                 // workgroups of one piece index
   float* part;                // [B Hkv tiles][pieces] slots of 2 x 64 x d floats
 };
@@ -29,6 +30,7 @@ struct BwdPlan {
   KeyPlan key;
   int shares;          // float: workgroups per query tile
   int qparts;          // workgroups of the query side per head
+  TileMap map;         // of the query side
   float* stat;         // what the key side needs of every query: float D, bf16 L and D as an operand (16 bytes)
   float* tpart;        // parts of the table's gradient, [B][H][qparts][buckets]
   size_t bytes;

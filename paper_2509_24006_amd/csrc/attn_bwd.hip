@@ -73,15 +73,16 @@ int dq_lds(const Attn& a) { return a.has_bias() ? DqLds<D>::BIAS + 5 * (2 * a.bi
 // (768 workgroups of up to 8 steps: 64 us with LDS atomics, 32 this way.)
 template <int D, bool BIAS>
 __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(Attn a, AttnGrads gr, RowStat* __restrict__ stats,
-                                                                                float* __restrict__ tpart, int tiles) {
+                                                                                float* __restrict__ tpart, TileMap map) {
   using Lds = DqLds<D>;
   using T = SwzTile<D>;
   constexpr int NT = D / 32, KT = D / 16, RB = 16 * T::ROW_BYTES;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 5, ln = l & 31;
   const int qh = w & 1, kh = w >> 1;
-  const BlockOf own = block_of(blockIdx.y, blockIdx.x, a.B * a.H, tiles);
+  const TileOf own = map.at(blockIdx.x);
   if (own.i < 0) return;
+  const int tiles = map.nb;
   const int bh = wave_uniform(own.bh), i = wave_uniform(a.causal ? tiles - 1 - own.i : own.i);   // (longest rows first)
   const int b = bh / a.H, h = bh - b * a.H, hk = h / a.G;
   const Seq s = seq_of(a, b);
@@ -382,7 +383,7 @@ __device__ __forceinline__ void store_keys(const Attn& a, const AttnGrads& gr, u
 }
 
 template <int D, bool BIAS>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkdv_kernel(Attn a, AttnGrads gr, const RowStat* __restrict__ stats, KeyPlan kp,
+__global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dkdv_kernel(Attn a, AttnGrads gr, const RowStat* __restrict__ stats, KeyPlan kp,
                                                             const float* __restrict__ tpart, int qparts) {
   using Lds = DkLds<D>;
   using T = SwzTile<D>;
@@ -395,8 +396,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkdv_kernel(Attn a,
   }
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 5, ln = l & 31;
   const int kh = w & 1, xh = w >> 1;
-  const int p = blockIdx.x / kp.blocks, bx = blockIdx.x - p * kp.blocks, brow = block_row(kp.tiles);
-  const BlockOf own = block_of(bx / brow, bx % brow, a.B * a.Hkv, kp.tiles);
+  const int p = blockIdx.x / kp.blocks, bx = blockIdx.x - p * kp.blocks;
+  const TileOf own = kp.map.at(bx);
   if (own.i < 0) return;
   const int bh = wave_uniform(own.bh), j = wave_uniform(own.i);
   const int b = bh / a.Hkv, hk = bh - b * a.Hkv;
@@ -669,7 +670,7 @@ hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_
     auto kern = a.has_bias() ? attn_dq_kernel<D, true> : attn_dq_kernel<D, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dq", st);
-    kern<<<dim3(block_row(p.qparts), block_rows(a.B * a.H, p.qparts)), 256, lds, st>>>(a, g, (RowStat*)p.stat, p.tpart, p.qparts);
+    kern<<<p.map.blocks(), 256, lds, st>>>(a, g, (RowStat*)p.stat, p.tpart, p.map);
   }
   const int tables = g.dtable ? a.H : 0, grid = p.key.blocks * p.key.pieces + tables;
   if (grid == 0) return hipGetLastError();

@@ -146,13 +146,14 @@ __device__ __forceinline__ void add_shares(f32x4* x, const f32x4 (&part)[NT], in
 
 template <int D, int QW, bool BIAS>
 __global__ __launch_bounds__(256, 2) void attn_f32_dq_kernel(Attn a, AttnGrads gr, float* __restrict__ Ds,
-                                                              float* __restrict__ tpart, int tiles) {
+                                                              float* __restrict__ tpart, TileMap map) {
   constexpr int NT = D / 16, TB = FTile<D>::BYTES, NQ = 4 / QW, NO = NT / QW, ROWS = kBlk / QW;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int tid = threadIdx.x, w = wave_uniform(tid >> 6), l = tid & 63, g = l >> 4, nl = l & 15;
   const int wk = w / QW, wq = w % QW;
-  const BlockOf own = block_of(blockIdx.y, blockIdx.x, a.B * a.H, tiles);
+  const TileOf own = map.at(blockIdx.x);
   if (own.i < 0) return;
+  const int tiles = map.nb;
   const int bh = wave_uniform(own.bh), i = wave_uniform(a.causal ? tiles - 1 - own.i : own.i);
   const int b = bh / a.H, h = bh - b * a.H, hk = h / a.G;
   const Seq s = seq_of(a, b);
@@ -417,7 +418,7 @@ hipError_t forward_impl(const Attn& a, const AttnPlan& plan, hipStream_t st) {
     return hipGetLastError();
   };
   if (!plan.parts) {
-    const dim3 grid(block_row(ow.tiles), block_rows(ow.units, ow.tiles));
+    const dim3 grid(plan.map.blocks());
     return launch(a.has_bias() ? attn_f32_fwd_kernel<D, true, false> : attn_f32_fwd_kernel<D, false, false>, grid, "attn_fwd");
   }
   return launch(a.has_bias() ? attn_f32_fwd_kernel<D, true, true> : attn_f32_fwd_kernel<D, false, true>,
@@ -448,7 +449,7 @@ hipError_t launch_dq(const Attn& a, const AttnGrads& g, const BwdPlan& p, hipStr
   auto kern = a.has_bias() ? attn_f32_dq_kernel<D, QW, true> : attn_f32_dq_kernel<D, QW, false>;
   SLA_TRY(ensure_dyn_lds(kern, lds));
   KernelTimer kt("attn_dq", st);
-  kern<<<dim3(block_row(p.qparts), block_rows(a.B * a.H, p.qparts)), 256, lds, st>>>(a, g, p.stat, p.tpart, p.qparts);
+  kern<<<p.map.blocks(), 256, lds, st>>>(a, g, p.stat, p.tpart, p.map);
   return hipGetLastError();
 }
 

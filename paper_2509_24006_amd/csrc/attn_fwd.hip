@@ -348,7 +348,7 @@ hipError_t forward_impl(const Attn& a, const AttnPlan& plan, hipStream_t st) {
     return hipGetLastError();
   };
   if (!plan.parts) {
-    const dim3 grid(block_row(ow.tiles), block_rows(ow.units, ow.tiles));
+    const dim3 grid(plan.map.blocks());
     return a.has_bias() ? launch(attn_fwd_kernel<D, true, false>, grid, "attn_fwd") : launch(attn_fwd_kernel<D, false, false>, grid, "attn_fwd");
   }
   const dim3 grid(plan.prefix.blocks + ow.blocks);

@@ -15,6 +15,7 @@ struct AttnPart {
 };
 struct AttnPlan {
   AttnPart prefix, own;   // (prefix.blocks = 0: none)
+  TileMap map;            // of `own`, where nothing is cut
   bool parts;             // sums in `part`, joined by a second launch
   long long slots;
   float *part, *stat;     // [slots][64][d], [slots][64][2]

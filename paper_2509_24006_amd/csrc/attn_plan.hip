@@ -47,6 +47,7 @@ AttnPlan attn_plan(const Attn& a, char* ws) {
   p.own.splits = (int)std::max(1ll, std::min(ceil_div(T, len), 256ll));
   p.prefix.splits = (int)std::max(1ll, std::min(ceil_div(Tp, len), 256ll));
   p.parts = a.Np > 0 || p.own.splits > 1;
+  p.map = tile_map(a, p.own.units, p.own.tiles);
   if (p.parts) {
     p.own.blocks = (int)(tiles * p.own.splits);
     p.prefix.blocks = (int)(ptiles * p.prefix.splits);
@@ -197,11 +198,13 @@ BwdPlan attn_bwd_plan(const Attn& a, char* ws) {
   const long long qunits = (long long)a.B * a.H * qtiles;
   p.shares = !f32 || qunits > 256 ? 1 : qunits > 128 ? 2 : 4;
   p.qparts = (a.Nq + kBlk / p.shares - 1) / (kBlk / p.shares);
+  p.map = tile_map(a, a.B * a.H, p.qparts);
   KeyPlan& k = p.key;
   k.tiles = (a.Nk + kBlk - 1) / kBlk;
   const long long units = (long long)a.B * a.Hkv * k.tiles;
   k.quarters = f32 ? (units < 384 ? 4 : 2) : 1;
-  k.blocks = units == 0 ? 0 : f32 ? (int)units * k.quarters : block_row(k.tiles) * block_rows(a.B * a.Hkv, k.tiles);
+  k.map = tile_map(a, a.B * a.Hkv, k.tiles);
+  k.blocks = f32 ? (int)units * k.quarters : k.map.blocks();
   const double slots = !f32 && a.d == 64 ? 768 : 512, wgs = (double)units * k.quarters, steps = (double)a.G * qtiles;
   double best = 1e300;
   k.pieces = 1;

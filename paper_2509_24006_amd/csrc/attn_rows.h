@@ -34,7 +34,7 @@ struct FwdTile {
       tile = x % pt.tiles;
       unit = x / pt.tiles;
     } else {
-      const BlockOf own = block_of(blockIdx.y, blockIdx.x, plan.own.units, plan.own.tiles);
+      const TileOf own = plan.map.at(blockIdx.x);
       if (own.i < 0) return false;
       unit = own.bh;
       tile = a.causal ? plan.own.tiles - 1 - own.i : own.i;   // (longest rows first)
