@@ -58,6 +58,12 @@ __device__ __forceinline__ int bucket_of(const Buckets& bk, int rel) {
 }
 __host__ __device__ inline int bucket_count(const Buckets& bk) { return (bk.n_borders + 1) * (bk.two_sided ? 2 : 1); }
 
+// A bias by distance lies in LDS for the distances -far .. far and a margin on both sides: a tile of 32 keys and 32
+// neighbouring queries that reaches into -far .. far reaches no further than 62 beyond, so that a value is found at its
+// distance without a comparison.
+constexpr int kBiasPad = 64;
+__host__ __device__ inline int bias_width(int far) { return 2 * (far + kBiasPad) + 1; }
+
 __device__ __forceinline__ float table_at(const Attn& a, int bucket, int h) {
   const size_t i = (size_t)bucket * a.H + h;
   return a.table16 ? to_f32(reinterpret_cast<const __hip_bfloat16*>(a.table)[i]) : reinterpret_cast<const float*>(a.table)[i];

@@ -61,21 +61,25 @@ __device__ __forceinline__ void table_part(const Attn& a, float* dist, int width
     dist[x] = t;
   }
   __syncthreads();
-  // bucket by bucket: the distances [n0, n1) of a side, the last bucket with the far sums
-  const int nb = bucket_count(a.bias), side = a.bias.n_borders + 1, u = tid;
-  if (u >= nb) return;
-  const bool right = u >= side;
-  const int v = right ? u - side : u;
-  const int n0 = v ? a.bias.borders[v - 1] : 0, n1 = v < side - 1 ? a.bias.borders[v] : far;
-  const float el = (ends[0] + ends[1]) + (ends[2] + ends[3]), er = (ends[4] + ends[5]) + (ends[6] + ends[7]);
+  // bucket by bucket, a power of two of neighbouring lanes each: the distances [n0, n1) of a side, the last bucket with the
+  // far sums
+  const int nb = bucket_count(a.bias), side = a.bias.n_borders + 1;
+  int share = 64;
+  while (share * nb > 256) share >>= 1;
+  const int u = tid / share, sub = tid & (share - 1);
   float t = 0.0f;
-  for (int x = right ? max(n0, 1) : n0; x < n1; ++x) t += dist[right ? far + x : far - x];
-  if (v == side - 1) t += right ? er : el;
-  if (!a.bias.two_sided && v == 0) {   // keys behind the query
-    for (int x = 1; x < far; ++x) t += dist[far + x];
-    t += er;
+  if (u < nb) {
+    const bool right = u >= side, first = u == 0 && !a.bias.two_sided;   // (one-sided: bucket 0 has the keys behind the query too)
+    const int v = right ? u - side : u;
+    const int n0 = v ? a.bias.borders[v - 1] : 0, n1 = v < side - 1 ? a.bias.borders[v] : far;
+    for (int x = (right ? max(n0, 1) : n0) + sub; x < n1; x += share) t += dist[right ? far + x : far - x];
+    if (first)
+      for (int x = 1 + sub; x < far; x += share) t += dist[far + x];
+    const float el = (ends[0] + ends[1]) + (ends[2] + ends[3]), er = (ends[4] + ends[5]) + (ends[6] + ends[7]);
+    if (sub == 0) t += (v == side - 1 ? (right ? er : el) : 0.0f) + (first ? er : 0.0f);
   }
-  out[u] = t;
+  for (int o = share >> 1; o; o >>= 1) t += __shfl_xor(t, o);
+  if (u < nb && sub == 0) out[u] = t;
 }
 
 // The gradient of one head's column of the table: the sum of the parts [b][tile], in an order fixed by their number.

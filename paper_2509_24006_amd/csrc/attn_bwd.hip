@@ -20,9 +20,10 @@ __device__ __forceinline__ BufDesc rows_rsrc(const View& v, int b, int h, int n)
   return tile_rsrc(p, (max(n, 1) - 1) * 2 * v.sn + 2 * D);
 }
 
-// bias in log2 units by distance, 2 far + 1 floats
+// bias in log2 units by distance
 __device__ __forceinline__ void expand_bias(const Attn& a, int h, float* out) {
-  for (int i = threadIdx.x; i <= 2 * a.bias.far; i += 256) out[i] = table_at(a, bucket_of(a.bias, i - a.bias.far), h) * kLog2e;
+  const int mid = a.bias.far + kBiasPad;
+  for (int i = threadIdx.x; i <= 2 * mid; i += 256) out[i] = table_at(a, bucket_of(a.bias, i - mid), h) * kLog2e;
 }
 
 // A query's L / scale and D, each as three bf16 terms (24 bits): the A operand of one more k-step of the key side's first
@@ -56,7 +57,9 @@ struct DqLds {
   static constexpr int BIAS = SKEW + 4 * 2048;
 };
 template <int D>
-int dq_lds(const Attn& a) { return a.has_bias() ? DqLds<D>::BIAS + 5 * (2 * a.bias.far + 1) * 4 + 32 : DqLds<D>::SKEW; }
+int dq_lds(const Attn& a) {
+  return a.has_bias() ? DqLds<D>::BIAS + bias_width(a.bias.far) * 4 + 4 * (2 * a.bias.far + 1) * 4 + 32 : DqLds<D>::SKEW;
+}
 
 // Wave (qh, kh): S^T and dP^T are [key][query], one query per lane, so L and D are per-lane scalars and dS^T feeds
 // dQ^T = K^T dS^T from registers.  The two kh waves hold sums over their keys and are added at the end.
@@ -64,7 +67,8 @@ int dq_lds(const Attn& a) { return a.has_bias() ? DqLds<D>::BIAS + 5 * (2 * a.bi
 // D: rowsum(dO O) has the rounding of O in it, which a sum of dS over many keys of a row (the last bucket of a bias) does not
 // average out, nor a row with few keys.  The sum of P (dP - D') over all keys is D - D' whatever D' is: the key side gets the
 // D that is corrected by it, and the last buckets' sums are corrected too.  dQ takes D' = rowsum(dO O) where there are
-// many keys, and otherwise (up to two tiles) D from a pass over them before.
+// many keys, and otherwise D from a pass over them before: one tile of them, or two where a bias makes probabilities less even
+// (with even scores its relative error from the rounding is 2^-9 over the root of the number of keys).
 //
 // The table's gradient is a sum of dS by distance.  Away from the diagonal a lane's values all belong to the last bucket
 // of a side, and stay in registers.  Near it the wave's 32 x 32 values are summed along their diagonals through LDS, 16 keys
@@ -112,9 +116,21 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
 #pragma unroll
     for (int t = 0; t < KT; ++t) of[t] = *reinterpret_cast<const bf16x8*>(o + 16 * t + 8 * g);
   }
+  const BufDesc descK = rows_rsrc<D>(a.K, b, hk, s.nk), descV = rows_rsrc<D>(a.V, b, hk, s.nk);
+  const std::integral_constant<int, 0> b0;   // the two pair buffers
+  const std::integral_constant<int, 1> b1;
+  auto issue = [&](int j, auto Buf) __attribute__((always_inline)) {
+    constexpr int O = decltype(Buf)::value * Lds::BUF;
+    tk.template load<O>(descK, j * tk.tile_step);
+    tv.template load<O + Lds::TILE>(descV, j * tv.tile_step);
+  };
+  if (steps > 0) issue(0, b0);
+  tk.pin();
+  tv.pin();
   float* const bias = reinterpret_cast<float*>(smem + Lds::BIAS);
   const int far = a.bias.far, width = 2 * far + 1;
-  float* const dist = bias + width;                    // [wave][width]
+  float* const dist = bias + bias_width(far);          // [wave][width]
+  const float* const bmid = bias + far + kBiasPad;     // at distance 0
   float* const skew = reinterpret_cast<float*>(smem + Lds::SKEW) + 512 * w;
   float* const stat = reinterpret_cast<float*>(smem + Lds::STAT);   // [kh][64]
   if constexpr (BIAS) {
@@ -133,17 +149,6 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
       gf[t] = lds_row(smem, qa.row(t) + Lds::BUF + Lds::TILE);
     }
   }
-  const BufDesc descK = rows_rsrc<D>(a.K, b, hk, s.nk), descV = rows_rsrc<D>(a.V, b, hk, s.nk);
-  const std::integral_constant<int, 0> b0;   // the two pair buffers
-  const std::integral_constant<int, 1> b1;
-  auto issue = [&](int j, auto Buf) __attribute__((always_inline)) {
-    constexpr int O = decltype(Buf)::value * Lds::BUF;
-    tk.template load<O>(descK, j * tk.tile_step);
-    tv.template load<O + Lds::TILE>(descV, j * tv.tile_step);
-  };
-  if (steps > 0) issue(0, b0);
-  tk.pin();
-  tv.pin();
   float dsum = 0.0f;
 #pragma unroll
   for (int t = 0; t < KT; ++t) {
@@ -204,12 +209,9 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
       near = __any(d0 + 31 > -far && d0 < far);
       if (near) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int x = min(max(d0 + c_row(r, g), -far), far) + far;
-          sT[r] = fast_exp2(fmaf(sT[r], sl2, bias[x] - Lq));
-        }
+        for (int r = 0; r < 16; ++r) sT[r] = fast_exp2(fmaf(sT[r], sl2, bmid[d0 + 4 * g + c_row(r, 0)] - Lq));
       } else {
-        const float bc = bias[d0 < 0 ? 0 : 2 * far] - Lq;
+        const float bc = bmid[d0 < 0 ? -far : far] - Lq;
 #pragma unroll
         for (int r = 0; r < 16; ++r) sT[r] = fast_exp2(fmaf(sT[r], sl2, bc));
       }
@@ -282,11 +284,11 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
     return stat[qh * 32 + ln] + stat[kBlk + qh * 32 + ln];
   };
   const std::integral_constant<bool, true> main;
-  if (steps <= 2 && steps > 0) {
+  if (steps > 0 && steps <= (BIAS ? 2 : 1)) {
     const std::integral_constant<bool, false> probe;
     nDq = 0.0f;
     step(probe, 0, b0);
-    if (steps > 1) step(probe, 1, b1);
+    if (BIAS && steps > 1) step(probe, 1, b1);
     dsum = both(drow);
     nDq = -dsum;
     drow = 0.0f;
@@ -454,6 +456,7 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dkdv_kerne
   if (cnt > 0) issue(b0);
   float* const bias = reinterpret_cast<float*>(smem + Lds::BIAS);
   const int far = a.bias.far;
+  const float* const bmid = bias + far + kBiasPad;   // at distance 0
   if constexpr (BIAS) expand_bias(a, ch, bias);
   wait_vm0_known();
   __syncthreads();
@@ -550,12 +553,9 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dkdv_kerne
     if constexpr (BIAS) {
       if (__any(e0 > -far && e0 - 31 < far)) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int x = min(max(e0 - c_row(r, g), -far), far) + far;
-          sm[r] = fast_exp2(fmaf(sm[r], sl2, bias[x]));
-        }
+        for (int r = 0; r < 16; ++r) sm[r] = fast_exp2(fmaf(sm[r], sl2, bmid[e0 - 4 * g - 27 + (27 - c_row(r, 0))]));
       } else {
-        const float bc = bias[e0 < 0 ? 0 : 2 * far];
+        const float bc = bmid[e0 < 0 ? -far : far];
 #pragma unroll
         for (int r = 0; r < 16; ++r) sm[r] = fast_exp2(fmaf(sm[r], sl2, bc));
       }
@@ -675,7 +675,7 @@ hipError_t backward_impl(const Attn& a, const AttnGrads& g, char* ws, hipStream_
   const int tables = g.dtable ? a.H : 0, grid = p.key.blocks * p.key.pieces + tables;
   if (grid == 0) return hipGetLastError();
   {
-    const int lds = DkLds<D>::BIAS + (a.has_bias() ? (2 * a.bias.far + 1) * 4 : 0);
+    const int lds = DkLds<D>::BIAS + (a.has_bias() ? bias_width(a.bias.far) * 4 : 0);
     auto kern = a.has_bias() ? attn_dkdv_kernel<D, true> : attn_dkdv_kernel<D, false>;
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt("attn_dkdv", st);

@@ -25,7 +25,7 @@ struct AttnLds {
   static constexpr int STAT = 4 * TILE;         // statistics of the four waves (1 KB)
   static constexpr int ROWQ = STAT + 1024;      // byte offsets of the 64 rows of Q (-1: none)
   static constexpr int ROWO = ROWQ + 256;       // offsets of the 64 rows of O in 16-byte units (-1: none)
-  static constexpr int BIAS = ROWO + 256;       // per head of the tile 2 far + 1 floats: bias in log2 units by distance
+  static constexpr int BIAS = ROWO + 256;       // per head of the tile: bias in log2 units by distance (bias_width floats)
 };
 
 // PART: the workgroup leaves sums for attn_join_kernel.
@@ -41,13 +41,48 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   FwdTile x;
   if (!x.template open<PART>(a, plan)) return;
   const AttnPart& pt = x.pre ? plan.prefix : plan.own;
+  const View &VK = x.pre ? a.Kp : a.K, &VV = x.pre ? a.Vp : a.V;
+  RunLoader<D> tk, tv;
+  tk.init(lds_base(smem), w, l, 2 * VK.sn, kBlk);
+  tv.init(lds_base(smem), w, l, 2 * VV.sn, kBlk);
+  constexpr int IPW = RunLoader<D>::IPW, QSLOT = 3 * Lds::TILE;
+  const int qr = T::RPI * w + l / T::CPR, chunk = ((l % T::CPR) ^ swz<D>(qr)) << 4;   // (Q: 16 rows or a multiple of it further
+  const unsigned ldsq = lds_base(smem) + QSLOT + wave_uniform(w) * 1024;              // with each load: the same swizzle)
+  // Loads of the tile's rows, and of the first two key tiles of a head, need no lengths: they are requested while the lengths
+  // are on their way.  Rows behind a sequence's queries come in like others (their results stay in their lanes and are
+  // written as zeros), and so do keys behind its length (their scores are replaced); rows of V behind it read as zeros.
+  // (2 x 12 heads x 512 tiles of 8 and 2 key tiles: 240 -> XX us.)
+  auto rsrc = [&](const View& v, int keys) {
+    return tile_rsrc(reinterpret_cast<const bf16*>(v.p) + x.key_at(v), (keys - 1) * 2 * v.sn + 2 * D);
+  };
+  BufDesc descK;
+  if constexpr (!PART) {
+    x.t0 = 0;
+    if (!pt.packed) {
+      const bf16* q = reinterpret_cast<const bf16*>(a.Q.p) + x.at(a.Q, RowOf{x.ub, 0, x.r0, true});
+      const BufDesc dq = tile_rsrc(q, (min(kBlk, a.Nq - x.r0) - 1) * 2 * a.Q.sn + 2 * D);
+#pragma unroll
+      for (int k = 0; k < IPW; ++k) load_to_lds16(dq, (qr + 4 * T::RPI * k) * 2 * a.Q.sn + chunk, 0, ldsq + 4096 * k);
+    }
+    descK = rsrc(VK, max(a.Nk, 1));
+    if (a.Nk > 0) tk.template load<0>(descK, 0);
+    if (a.Nk > kBlk) tk.template load<2 * Lds::TILE>(descK, tk.tile_step);
+  }
+  x.template range<PART>(a, pt);
   const int steps = x.steps, h0 = x.h0;
+  const BufDesc descV = rsrc(VV, x.keys());   // (up to the last valid one of this workgroup)
+  if constexpr (PART) {
+    descK = rsrc(VK, x.keys());
+    if (steps > 0) tk.template load<0>(descK, 0);
+    if (steps > 1) tk.template load<2 * Lds::TILE>(descK, tk.tile_step);
+  }
+  if (steps > 0) tv.template load<Lds::TILE>(descV, 0);
   const RowOf row = x.row(a, pt, qh * 32 + ln);   // this lane's
   const RowKeys rk = row_keys(a, x, row);
   const bool live = rk.live;
   const int posk = rk.pos, lim = rk.lim;
   // 32-bit offsets of the tile's rows, from the unit's first row or, where a unit is one head, the tile's
-  RowOf first = {max(x.ub, 0), 0, pt.packed ? 0 : x.r0, true};
+  const RowOf first = {max(x.ub, 0), 0, pt.packed ? 0 : x.r0, true};
   const long long qbase = x.at(a.Q, first), obase = x.at(a.O, first);
   int* const rowq = reinterpret_cast<int*>(smem + Lds::ROWQ);
   int* const rowo = reinterpret_cast<int*>(smem + Lds::ROWO);
@@ -57,44 +92,26 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
     rowo[tid] = r.in ? (int)((x.at(a.O, r) - obase) >> 3) : -1;
   }
   float* const bias = reinterpret_cast<float*>(smem + Lds::BIAS);
-  const int far = a.bias.far, width = 2 * far + 1;
+  const int far = a.bias.far, width = bias_width(far);
   if constexpr (BIAS) {
     for (int i = tid; i < pt.heads * width; i += 256) {
       const int hg = i / width;
-      bias[i] = table_at(a, bucket_of(a.bias, i - hg * width - far), h0 + hg) * kLog2e;
+      bias[i] = table_at(a, bucket_of(a.bias, i - hg * width - far - kBiasPad), h0 + hg) * kLog2e;
     }
   }
-  __syncthreads();
-
+  if (PART || pt.packed) {
+    __syncthreads();
+    const BufDesc dq = tile_rsrc(reinterpret_cast<const bf16*>(a.Q.p) + qbase, 0x7fff0000);
+#pragma unroll
+    for (int k = 0; k < IPW; ++k) {
+      const int o = rowq[qr + 4 * T::RPI * k];
+      load_to_lds16(dq, o < 0 ? (int)kPastEnd : o + chunk, 0, ldsq + 4096 * k);
+    }
+  }
   f32x16 oT[NT];
 #pragma unroll
   for (int et = 0; et < NT; ++et) oT[et] = zero_f32x16();
   float m = -INFINITY, lsum = 0.0f;
-  const View &VK = x.pre ? a.Kp : a.K, &VV = x.pre ? a.Vp : a.V;
-  RunLoader<D> tk, tv;
-  tk.init(lds_base(smem), w, l, 2 * VK.sn, kBlk);
-  tv.init(lds_base(smem), w, l, 2 * VV.sn, kBlk);
-  constexpr int IPW = RunLoader<D>::IPW;
-  // the descriptors span this workgroup's keys up to the last valid one: rows behind it read as zeros
-  auto rsrc = [&](const View& v) {
-    return tile_rsrc(reinterpret_cast<const bf16*>(v.p) + x.key_at(v), (x.keys() - 1) * 2 * v.sn + 2 * D);
-  };
-  const BufDesc descK = rsrc(VK), descV = rsrc(VV);
-  constexpr int QSLOT = 3 * Lds::TILE;
-  {
-    const BufDesc dq = tile_rsrc(reinterpret_cast<const bf16*>(a.Q.p) + qbase, 0x7fff0000);
-    const int qr = T::RPI * w + l / T::CPR, chunk = ((l % T::CPR) ^ swz<D>(qr)) << 4;
-#pragma unroll
-    for (int k = 0; k < IPW; ++k) {   // (16 rows or a multiple of it further each time: the same swizzle)
-      const int o = rowq[qr + 4 * T::RPI * k];
-      load_to_lds16(dq, o < 0 ? (int)kPastEnd : o + chunk, 0, lds_base(smem) + QSLOT + wave_uniform(w) * 1024 + 4096 * k);
-    }
-  }
-  if (steps > 0) {
-    tk.template load<0>(descK, 0);
-    tv.template load<Lds::TILE>(descV, 0);
-    if (steps > 1) tk.template load<2 * Lds::TILE>(descK, tk.tile_step);
-  }
   // per-lane LDS offsets of the operand reads inside a tile; accumulator tile et holds feature tile et ^ rot: the half
   // of the features that the wave finishes by itself comes first
   const int rot = wave_uniform(par) * HT;
@@ -120,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   // The scores of a step are formed one step ahead: their products run under the exponentials of the current step.
   f32x16 sT = zero_f32x16();
   bf16x8 qf[KT], k0[KT];
-  if (steps > 1) wait_vm<2 * IPW>();   // Q and K_0 have landed; V_0 and K_1 may stay in flight
+  if (!PART && !pt.packed && steps > 1) wait_vm<2 * IPW>();   // Q and K_0 have landed; K_1 and V_0 may stay in flight
   else wait_vm0();
   __syncthreads();
   {
@@ -148,7 +165,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
     __syncthreads();
   }
   const float cs = BIAS ? 1.0f : c2;              // the scores' factor in the exponent of 2
-  const float* const brow = bias + (BIAS ? row.g * width : 0);
+  const float* const brow = bias + (BIAS ? row.g * width + far + kBiasPad : 0);   // at distance 0
   int key0 = x.t0 * kBlk + 32 * wave_uniform(par);  // first key of this wave in the current tile
   int koff = 3 * tk.tile_step, voff = 2 * tv.tile_step;
   // One step; P = parity of s.  On entry K_{s+1} and V_s are in their slots for every wave and sT holds S_s; sN
@@ -171,13 +188,12 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
       // Distances of far and more share a bucket: away from the diagonal the bias is one value per row.
       const int d0 = key0 - posk;   // distance of this wave's first key
       if (__any(d0 + 31 > -far && d0 < far)) {
+        // (queries of a packed tile may be far apart; those of others are neighbours, within the padding)
+        const float* const b0 = brow + (PART || pt.packed ? min(max(d0, -far - 31), far) : d0) + 4 * g;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int i = min(max(d0 + c_row(r, g), -far), far) + far;
-          sT[r] = fmaf(sT[r], c2, brow[i]);
-        }
+        for (int r = 0; r < 16; ++r) sT[r] = fmaf(sT[r], c2, b0[c_row(r, 0)]);
       } else {
-        const float bc = brow[d0 < 0 ? 0 : 2 * far];
+        const float bc = brow[d0 < 0 ? -far : far];
 #pragma unroll
         for (int r = 0; r < 16; ++r) sT[r] = fmaf(sT[r], c2, bc);
       }
@@ -341,7 +357,7 @@ hipError_t forward_impl(const Attn& a, const AttnPlan& plan, hipStream_t st) {
   const float c2 = a.scale * kLog2e;
   const AttnPart& ow = plan.own;
   auto launch = [&](auto kern, dim3 grid, const char* name) -> hipError_t {
-    const int lds = AttnLds<D>::BIAS + (a.has_bias() ? ow.heads * (2 * a.bias.far + 1) * 4 : 0);
+    const int lds = AttnLds<D>::BIAS + (a.has_bias() ? ow.heads * bias_width(a.bias.far) * 4 : 0);
     SLA_TRY(ensure_dyn_lds(kern, lds));
     KernelTimer kt(name, st);
     kern<<<grid, 256, lds, st>>>(a, plan, c2);

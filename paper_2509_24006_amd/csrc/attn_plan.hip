@@ -33,7 +33,7 @@ AttnPlan attn_plan(const Attn& a, char* ws) {
   AttnPlan p = {};
   // The heads of a group share a row tile where one head's queries would leave most of it empty.  (Their bias takes
   // LDS per head: as many as leave room for two workgroups on a CU, else one.)
-  const long long bias = a.has_bias() ? a.G * (2ll * a.bias.far + 1) * 4 : 0;
+  const long long bias = a.has_bias() ? a.G * 4ll * bias_width(a.bias.far) : 0;
   const bool packed = (a.Nq < kBlk || a.Np > 0) && bias <= 12 * 1024;
   const int heads = packed ? a.G : 1;
   p.own = part_of(a.B * a.H / heads, heads, (long long)heads * a.Nq, packed);

@@ -117,6 +117,15 @@ def test_position_bias(dt, table_dtype, bias, B, H, Hkv, N, d, causal):
 
 
 @pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("bias", [(8, 20, True), (4, 3, False), (16, 40, True)])
+@pytest.mark.parametrize("Nq,Nk,causal", [(70, 90, False), (90, 70, True), (250, 250, False), (65, 400, True), (129, 64, False)])
+def test_bias_whose_last_distance_is_within_a_tile(dt, bias, Nq, Nk, causal):
+    # tiles that lie on one side of the diagonal as a whole, and last tiles of a few rows
+    check(dt, 2, 4, 2, Nq, Nk, 64, causal, None, [Nk, Nk // 3], bias)
+    check(dt, 1, 2, 2, Nq, Nk, 128, causal, [Nq - 3], None, bias)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
 def test_bias_of_a_rectangle(dt):
     check(dt, 2, 2, 2, 40, 333, 64, bias=(32, 128, True))
     check(dt, 2, 2, 2, 333, 40, 64, causal=True, bias=(8, 20, False))
