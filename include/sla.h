@@ -196,7 +196,8 @@ int sla_aggregate_states(const sla_params* p, int method, const void* luts, cons
 
 /* Buckets of the distance r = kp - (n + q0(b)).  With m = |r| (two_sided) or max(-r, 0): bucket = number of borders
  * <= m, plus n_buckets / 2 where two_sided and r > 0.  n_buckets = 0: no bias.  A side has n_buckets (two_sided:
- * n_buckets / 2) buckets, at most 64, and one border less; borders ascend from 1 at least to SLA_ATTN_MAX_DISTANCE. */
+ * n_buckets / 2) buckets, at most 64, and one border less; borders ascend from 1 at least to SLA_ATTN_MAX_DISTANCE.  Table
+ * entries of -1e30 and below hide their pairs: a key that a row sees only through them does not exist for it. */
 enum { SLA_ATTN_BORDERS = 63, SLA_ATTN_MAX_DISTANCE = 1024 };
 typedef struct sla_buckets {
   int32_t n_buckets, two_sided;

@@ -64,9 +64,12 @@ __host__ __device__ inline int bucket_count(const Buckets& bk) { return (bk.n_bo
 constexpr int kBiasPad = 64;
 __host__ __device__ inline int bias_width(int far) { return 2 * (far + kBiasPad) + 1; }
 
+// An entry of -1e30 and below is a mask, a type's lowest value among them: beside it a score has no bits left, and its
+// logarithm to base 2 may not be finite.
 __device__ __forceinline__ float table_at(const Attn& a, int bucket, int h) {
   const size_t i = (size_t)bucket * a.H + h;
-  return a.table16 ? to_f32(reinterpret_cast<const __hip_bfloat16*>(a.table)[i]) : reinterpret_cast<const float*>(a.table)[i];
+  const float x = a.table16 ? to_f32(reinterpret_cast<const __hip_bfloat16*>(a.table)[i]) : reinterpret_cast<const float*>(a.table)[i];
+  return x <= -1e30f ? -INFINITY : x;
 }
 
 // Which head and tile a workgroup of a launch over BH heads of nb tiles owns.  Workgroups are dealt to the 8 XCDs (each with

@@ -185,7 +185,8 @@ __global__ __launch_bounds__(256, 2) void attn_f32_dq_kernel(Attn a, AttnGrads g
     Dr = dot_frag<NT>(gf, of);
     if (live && g == 0 && wq == 0) Ds[(size_t)bh * a.Nq + n] = Dr;
   }
-  const float Lr = live ? a.L[(size_t)bh * a.Nq + n] : 0.0f;
+  float Lr = live ? a.L[(size_t)bh * a.Nq + n] : 0.0f;
+  if (Lr == -INFINITY) Lr = INFINITY;   // (a row without a key: P = 0)
   float* const bias = reinterpret_cast<float*>(smem + 2 * TB);
   const int far = a.bias.far, width = 2 * far + 1;
   float* const dist = bias + width;   // [wave][width], then the far sums of the waves
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void attn_f32_key_kernel(Attn a, AttnGrads 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int nq = i * kBlk + 16 * (NQ * wq + q) + 4 * g + r, d = key - (sq.pos + nq);
-          float v = pr[q][r] * a.scale - Lr[r];
+          float v = pr[q][r] * a.scale - (Lr[r] == -INFINITY ? INFINITY : Lr[r]);
           if constexpr (BIAS) v += bias_at(bias, far, d);
           pr[q][r] = nq < sq.nq && !(a.causal && d > 0) ? expf(v) : 0.0f;
           dp[q][r] = pr[q][r] * (dp[q][r] - Dr[r]);

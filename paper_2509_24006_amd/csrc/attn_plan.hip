@@ -68,10 +68,12 @@ bool attn_forward_fits(const Attn& a) {
   constexpr long long lim = (1ll << 31) - (1 << 17);
   const long long esz = a.dtype == SLA_F32 ? 4 : 2;
   // keys of one workgroup behind one descriptor
-  auto span = [&](const View& v, long long tiles, int splits) { return (ceil_div(tiles, splits) + 1) * kBlk * v.sn * esz; };
+  auto span = [&](const View& v, long long n, long long tiles, int splits) {
+    return std::min(n, (ceil_div(tiles, splits) + 1) * kBlk) * v.sn * esz;
+  };
   const long long T = ceil_div(a.Nk, kBlk), Tp = ceil_div(a.Np, kBlk);
-  if (span(a.K, T, p.own.splits) >= lim || span(a.V, T, p.own.splits) >= lim) return false;
-  if (a.Np && (span(a.Kp, Tp, p.prefix.splits) >= lim || span(a.Vp, Tp, p.prefix.splits) >= lim)) return false;
+  if (span(a.K, a.Nk, T, p.own.splits) >= lim || span(a.V, a.Nk, T, p.own.splits) >= lim) return false;
+  if (a.Np && (span(a.Kp, a.Np, Tp, p.prefix.splits) >= lim || span(a.Vp, a.Np, Tp, p.prefix.splits) >= lim)) return false;
   // rows of a packed unit (those of one head are counted from their tile)
   if (p.own.packed || a.Np) {
     auto rows = [&](const View& v) { return ((a.Np ? a.B - 1 : 0) * v.sb + (p.own.heads - 1) * v.sh + (long long)(a.Nq - 1) * v.sn + a.d) * esz; };

@@ -391,14 +391,12 @@ struct DenseAttention : torch::autograd::Function<DenseAttention> {
   static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& Q, const at::Tensor& K,
                                                 const at::Tensor& V, const std::optional<at::Tensor>& table,
                                                 const at::Tensor* q_len, const at::Tensor* k_len, const sla_attn_params* p,
-                                                bool token, void* st) {
-    at::Tensor O, L;
-    const at::Tensor none, &tb = table ? *table : none;
-    TORCH_CHECK(attend_forward(*p, token, Q, K, V, nullptr, nullptr, defined(tb), q_len, k_len, st, &O, &L), "sla_attn_forward failed");
-    ctx->save_for_backward({Q, K, V, tb, O, L, q_len ? *q_len : none, k_len ? *k_len : none});
+                                                bool token, const at::Tensor* O, const at::Tensor* L) {   // (the call is made already)
+    const at::Tensor none;
+    ctx->save_for_backward({Q, K, V, table ? *table : none, *O, *L, q_len ? *q_len : none, k_len ? *k_len : none});
     ctx->saved_data["p"] = std::string(reinterpret_cast<const char*>(p), sizeof(*p));
     ctx->saved_data["token"] = token;
-    return {O};
+    return {*O};
   }
   static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
     const auto s = ctx->get_saved_variables();
@@ -453,7 +451,7 @@ struct DenseAttention : torch::autograd::Function<DenseAttention> {
       if (out.size() > 3) dT = out[3];
     }
     const at::Tensor no;
-    return {dQ, dK, dV, dT, no, no, no, no, no};
+    return {dQ, dK, dV, dT, no, no, no, no, no, no};
   }
 };
 
@@ -485,33 +483,17 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   bool grad = false;
   if (!at_.cached && c10::GradMode::is_enabled())
     for (int i : {0, 1, 2, 5}) grad = grad || (t[i] && t[i]->requires_grad());
-  if (grad) {
-    // (checked first: the node's own forward call may not fail half way)
-    AttnCall c;
-    sla_tensor x;
-    const void* tb;
-    const int32_t* len;
-    const int64_t q = 16 / Q.element_size();
-    bool ok = c.open(&p, at_.token, &Q) && c.table(t[5], &tb) && c.lengths(t[6], &len) && c.lengths(t[7], &len);
-    for (int i = 0; ok && i < 3; ++i) {
-      const int heads = i ? p.Hkv : p.H, rows = i ? p.Nk : p.Nq;
-      ok = c.rows(t[i], heads, rows, &x) && reinterpret_cast<uintptr_t>(x.data) % 16 == 0 &&
-           (p.B < 2 || x.stride_b % q == 0) && (heads < 2 || x.stride_h % q == 0) &&
-           (rows < 2 || (x.stride_n % q == 0 && x.stride_n >= p.d && x.stride_n * Q.element_size() <= 1 << 24 &&
-                         rows * x.stride_n * Q.element_size() < 1ll << 31));
-    }
-    if (!ok) Py_RETURN_NONE;
-    O = DenseAttention::apply(Q, K, V, t[5] ? std::optional<at::Tensor>(*t[5]) : std::nullopt, t[6], t[7],
-                              static_cast<const sla_attn_params*>(&p), at_.token, st)[0];
-  } else {
+  at::Tensor L;
+  {
     const at::NoGradGuard no;
-    bool ok;
-    {
-      NoGil free;
-      ok = attend_forward(p, at_.token, Q, K, V, t[3], t[4], t[5], t[6], t[7], st, &O, nullptr);
-    }
-    if (!ok) Py_RETURN_NONE;
+    NoGil free;
+    if (!attend_forward(p, at_.token, Q, K, V, t[3], t[4], t[5], t[6], t[7], st, &O, grad ? &L : nullptr)) O = at::Tensor();
   }
+  if (!O.defined()) Py_RETURN_NONE;
+  if (grad)
+    O = DenseAttention::apply(Q, K, V, t[5] ? std::optional<at::Tensor>(*t[5]) : std::nullopt, t[6], t[7],
+                              static_cast<const sla_attn_params*>(&p), at_.token, static_cast<const at::Tensor*>(&O),
+                              static_cast<const at::Tensor*>(&L))[0];
   return THPVariable_Wrap(O);
   END_HANDLE_TH_ERRORS
 }

@@ -46,8 +46,11 @@ def attention(Q, K, V, scale, causal=False, q_len=None, k_len=None, pos=None, ta
             mag = (q.abs() @ k.abs().T) * scale * (d + 2)     # times e: error of the float scores
             if table is not None:
                 bk = bucket(rel, list(borders), two_sided)
-                S = S + table.double()[:, h][bk]
-                mag = mag + 2 * table.double()[:, h][bk].abs()
+                t = table.double()[:, h][bk]
+                seen = seen & (t > -1e30)                     # (lower entries hide their pairs)
+                t = torch.where(seen, t, torch.zeros_like(t))
+                S = S + t
+                mag = mag + 2 * t.abs()
             S = S.masked_fill(~seen, -torch.inf)
             L = torch.logsumexp(S, 1, keepdim=True)
             some = seen.any(1, keepdim=True)

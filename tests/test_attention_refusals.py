@@ -96,6 +96,12 @@ def test_bias_and_prefix_refusals():
     assert _call(long, fwd=False, bytes=BIG, K=far) == -2                             # a head of 2^33 bytes
 
 
+def test_offsets_past_32_bits_are_refused():
+    far = dict(sn=1 << 12)                                                            # rows 8 KB apart
+    assert _call(_params(B=1, H=8, Hkv=8, Nq=1 << 15, Nk=1 << 19), bytes=BIG, K=far) == -2   # a head of 4 GB through one workgroup
+    assert _call(_params(B=1 << 12, H=1, Hkv=1, Nq=1, Nk=1, Np=5), bytes=BIG, Kp=dict(), Vp=dict(), Q=dict(sb=1 << 19)) == -2
+
+
 def test_binding_refuses_wrong_tensors():
     from paper_2509_24006_amd import autograd as attn
     q = torch.zeros(1, 2, 3, 64)

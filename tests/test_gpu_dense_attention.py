@@ -149,6 +149,38 @@ def test_one_key_takes_everything():
     within(O, want["O"], "O")
 
 
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("low", [-math.inf, "lowest", -1e30])
+@pytest.mark.parametrize("causal", [False, True])
+def test_table_entries_that_hide_their_pairs(dt, low, causal):
+    Q, K, V, dO = tensors(dt, 2, 3, 1, 150, 150, 64)
+    bk = sla.position_buckets(8, 20, True)
+    table = torch.randn(8, 3, device="cuda").to(dt)
+    low = torch.finfo(dt).min if low == "lowest" else low
+    table[2, 0] = table[5:, 1] = low
+    table[:, 2] = low                  # nothing is left for the third head
+    table[1, 2] = 0.5                  # but one distance
+    want = ref.attention(Q, K, V, 0.125, causal, pos=[0, 0], table=table, borders=list(bk.borders)[:3], two_sided=True, dO=dO, result=dt)
+    leaves = [t.clone().requires_grad_(True) for t in (Q, K, V, table)]
+    O = attn.dense_attention(*leaves[:3], causal=causal, table=leaves[3], buckets=bk)
+    within(O, want["O"], "O")
+    assert float(O.detach()[:, 2, 0].abs().max()) == 0 or not causal   # (its only key would be itself)
+    for name, got in zip(("dQ", "dK", "dV", "dtable"), torch.autograd.grad(O, leaves, dO)):
+        within(got, want[name], name)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+def test_no_keys_at_all(dt):
+    Q, K, V, dO = tensors(dt, 2, 4, 2, 70, 0, 64)
+    table, bk = torch.randn(8, 4, device="cuda"), sla.position_buckets(8, 20)
+    leaves = [t.clone().requires_grad_(True) for t in (Q, K, V, table)]
+    O = attn.dense_attention(*leaves[:3], table=leaves[3], buckets=bk)
+    got = torch.autograd.grad(O, leaves, dO)
+    assert float(O.detach().abs().max()) == 0 and float(got[0].abs().max()) == 0 and float(got[3].abs().max()) == 0
+    assert got[1].shape == K.shape
+    assert float(attn.cached_attention(Q[:, :, :3], K, V).abs().max()) == 0
+
+
 # ---------------------------------------------------------------- serving
 
 def serve(dt, B, H, Hkv, Nq, Nk, d, k_len=None, Np=0, bias=None, token=False, causal=True, seed=0, garbage=True):
@@ -178,7 +210,8 @@ def serve(dt, B, H, Hkv, Nq, Nk, d, k_len=None, Np=0, bias=None, token=False, ca
 @pytest.mark.parametrize("token", [False, True], ids=["head_major", "token_major"])
 @pytest.mark.parametrize("B,H,Hkv,Nq,Nk,d,k_len", [
     (1, 2, 2, 1, 1, 64, None), (1, 12, 12, 1, 1000, 128, None), (5, 8, 2, 1, 700, 128, [700, 1, 0, 333, 64]),
-    (3, 4, 1, 5, 300, 64, [300, 5, 2]), (2, 6, 2, 70, 500, 64, [500, 70]), (4, 16, 1, 8, 2000, 128, [2000, 9, 8, 1500])])
+    (3, 4, 1, 5, 300, 64, [300, 5, 2]), (2, 6, 2, 70, 500, 64, [500, 70]), (4, 16, 1, 8, 2000, 128, [2000, 9, 8, 1500]),
+    (2, 128, 1, 1, 300, 64, [1 << 20, -5]), (3, 5, 5, 63, 1500, 64, [1500, 70, 63])])
 def test_new_tokens_over_a_cache(dt, token, B, H, Hkv, Nq, Nk, d, k_len):
     serve(dt, B, H, Hkv, Nq, Nk, d, k_len, token=token)
 
@@ -232,6 +265,106 @@ def test_slices_of_a_fused_projection_and_broadcast_heads(dt):
     mag = (want["dK"][0].abs() + want["dV"][0].abs()).sum((0, 1), keepdim=True)
     bound = (want["dK"][1] + want["dV"][1]).sum((0, 1), keepdim=True) + 3 * ref.U[dt] * mag
     within(g, (both.sum((0, 1), keepdim=True), bound), "shared K, V")
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("Nq", [3, 90])
+def test_every_tensor_has_strides_of_its_own(dt, Nq):
+    Q, K, V, dO = tensors(dt, 2, 4, 2, Nq, 130, 64)
+    want = attn.dense_attention(Q, K, V)
+    turned = lambda t: t.transpose(1, 2).contiguous().transpose(1, 2)
+    kv = torch.stack([V, K, V], 3)
+    variants = [(turned(Q), K, kv[:, :, :, 2]), (Q, kv[:, :, :, 1], turned(V)), (turned(Q), turned(K), V)]
+    plain = [t.clone().requires_grad_(True) for t in (Q, K, V)]
+    grads = torch.autograd.grad(attn.dense_attention(*plain), plain, dO)
+    for q, k, v in variants:
+        assert not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous())
+        ls = [t.detach().requires_grad_(True) for t in (q, k, v)]
+        O = attn.dense_attention(*ls)
+        assert torch.equal(O, want)
+        assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(O, ls, turned(dO)), grads))
+
+
+def test_rows_sixteen_megabytes_apart():
+    room = torch.empty(70 << 23, dtype=BF, device="cuda")   # 70 rows of 16 MB
+    far = room.as_strided((1, 1, 70, 64), (0, 0, 1 << 23, 1))
+    Q, K, V, dO = tensors(BF, 1, 1, 1, 70, 70, 64)
+    plain = [t.clone().requires_grad_(True) for t in (Q, K, V)]
+    O = attn.dense_attention(*plain, causal=True)
+    want = (O.detach(),) + torch.autograd.grad(O, plain, dO)
+    for i in range(3):
+        far.copy_(plain[i].detach())
+        ls = [t.detach().requires_grad_(True) for t in plain]
+        ls[i] = far.detach().requires_grad_(True)
+        O = attn.dense_attention(*ls, causal=True)
+        got = (O.detach(),) + torch.autograd.grad(O, ls, dO)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_a_head_that_spans_more_than_two_gigabytes():
+    # [B, N, H, d] with 2.2 GB from a head's first row to its last
+    N, Hall = 140000, 64
+    K, V = (torch.zeros(1, N, Hall, 128, dtype=BF, device="cuda")[:, :, 5:7] for _ in range(2))
+    g = torch.Generator("cuda").manual_seed(3)
+    for t in (K, V):
+        t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+    K[:, 139990:] *= 4
+    Q = torch.randn(1, 2, 4, 128, generator=g, device="cuda").to(BF)
+    lens = ints([139997])
+    O = attn.cached_attention(Q, K, V, lens, token_major=True)
+    h = lambda t: t.transpose(1, 2)
+    want = ref.attention(h(Q), h(K), h(V), 128 ** -0.5, True, None, [139997], [139995])
+    within(h(O), want["O"], "O")
+    # many queries go through one workgroup's 32-bit offsets: refused, not wrong
+    with pytest.raises(sla.SLAError, match="unsupported"):
+        attn.dense_attention(torch.zeros(1, 64 * 512, 4, 128, dtype=BF, device="cuda"), K, V, token_major=True)
+
+
+def test_another_stream():
+    Q, K, V, dO = tensors(BF, 2, 4, 2, 200, 200, 64)
+    ls = [t.clone().requires_grad_(True) for t in (Q, K, V)]
+    O = attn.dense_attention(*ls, causal=True)
+    want = (O.detach(),) + torch.autograd.grad(O, ls, dO)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        busy = torch.randn(2048, 2048, device="cuda")
+        for _ in range(20):
+            busy = busy @ busy * 1e-3
+        ls = [(t + 0).requires_grad_(True) for t in (Q, K, V)]   # made on this stream, behind its work
+        O = attn.dense_attention(*ls, causal=True)
+        got = (O.detach(),) + torch.autograd.grad(O, ls, dO)
+        serve_ = attn.cached_attention(Q[:, :, :2] + 0, K, V)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.equal(serve_, attn.cached_attention(Q[:, :, :2].contiguous(), K, V))
+
+
+def test_wrong_tensors_are_refused_on_the_device():
+    Q, K, V, dO = tensors(BF, 2, 4, 2, 10, 20, 64)
+    bk, table = sla.position_buckets(8, 20), torch.randn(8, 4, device="cuda")
+    for kw in (dict(k_len=torch.tensor([20, 20], device="cuda")), dict(k_len=ints([20])), dict(k_len=torch.tensor([20, 20], dtype=torch.int32)),
+               dict(table=table[:, :3].contiguous(), buckets=bk), dict(table=table.half(), buckets=bk), dict(table=table),
+               dict(buckets=bk), dict(scale=-1.0), dict(scale=math.nan)):
+        with pytest.raises(sla.SLAError):
+            attn.dense_attention(Q, K, V, **kw)
+        with pytest.raises(sla.SLAError):
+            attn.dense_attention(Q.clone().requires_grad_(True), K, V, **kw)
+    for bad in ((Q, K[:, :, :5], V), (Q, K, V[..., :32]), (Q, K.float(), V), (Q[:1], K, V), (Q[:, :3], K, V), (Q, K.cpu(), V),
+                (Q[..., :48].contiguous(), K[..., :48].contiguous(), V[..., :48].contiguous())):
+        with pytest.raises(sla.SLAError):
+            attn.dense_attention(*bad)
+    with pytest.raises(sla.SLAError):
+        attn.cached_attention(Q, K, V, prefix=(K[0], V[0, :1]))
+
+
+def test_many_short_sequences():
+    Q, K, V, _ = tensors(BF, 4000, 16, 4, 1, 30, 64)
+    lens = torch.arange(4000, device="cuda", dtype=torch.int32) % 31
+    O = attn.cached_attention(Q, K, V, lens)
+    at = [0, 1, 30, 31, 2047, 3999]
+    want = ref.attention(Q[at], K[at], V[at], 0.125, True, None, [x % 31 for x in at], [x % 31 - 1 for x in at])
+    within(O[at], want["O"], "O")
 
 
 @pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
@@ -338,6 +471,39 @@ def test_captured_calls_replay(which):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
     assert len(eager_side) == len(held)
+
+
+def test_a_captured_training_step_replays():
+    """forward and backward through autograd inside a graph, on leaves that no other graph uses"""
+    bk = sla.position_buckets(8, 20)
+    new = lambda: [t.clone().requires_grad_(True) for t in tensors(BF, 2, 4, 2, 90, 150, 64)[:3]] + [
+        torch.randn(8, 4, device="cuda", generator=torch.Generator("cuda").manual_seed(9)).requires_grad_(True)]
+    dO = torch.randn(2, 4, 90, 64, device="cuda").to(BF)
+
+    def step(ls):
+        O = attn.dense_attention(*ls[:3], table=ls[3], buckets=bk)
+        return (O.detach(),) + torch.autograd.grad(O, ls, dO)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(new())
+    torch.cuda.current_stream().wait_stream(side)
+    held_leaves = new()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step(held_leaves)
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        with torch.no_grad():
+            for t in held_leaves + [dO]:
+                t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        want = step([t.detach().clone().requires_grad_(True) for t in held_leaves])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
 
 
 def test_tensor_subclasses_go_through_the_checked_calls():
