@@ -351,7 +351,8 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
 // feature half x, over all 64 queries.  P and dS cross between the two waves of a key half through LDS in operand layout.
 // L and D of a query enter the first products as one more k-step (row_stat).  What counts is the number of instructions
 // (a wave issues one in five cycles or more): loads with one M0 a tile, descriptors that change with the head only, L and
-// D as a ready operand.  (XX)
+// D as a ready operand.  (Instructions of a step 414 -> 290 at d = 128, 337 -> 240 at d = 64; key side of 256 heads x 1024,
+// d = 64, 221 -> 195 us, of 12 x 32760, d = 128, 12.58 -> 12.19 ms.)
 template <int D>
 struct DkLds {
   static constexpr int TILE = SwzTile<D>::BYTES;

@@ -32,7 +32,6 @@ __global__ __launch_bounds__(256, 2) void attn_f32_fwd_kernel(Attn a, AttnPlan p
   FwdTile x;
   if (!x.template open<PART>(a, plan)) return;
   const AttnPart& pt = x.pre ? plan.prefix : plan.own;
-  x.template range<PART>(a, pt);
   const RowOf row = x.row(a, pt, 16 * w + n);
   const RowKeys rk = row_keys(a, x, row);
   const View &VK = x.pre ? a.Kp : a.K, &VV = x.pre ? a.Vp : a.V;

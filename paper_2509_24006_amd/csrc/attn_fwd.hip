@@ -41,42 +41,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   FwdTile x;
   if (!x.template open<PART>(a, plan)) return;
   const AttnPart& pt = x.pre ? plan.prefix : plan.own;
-  const View &VK = x.pre ? a.Kp : a.K, &VV = x.pre ? a.Vp : a.V;
-  RunLoader<D> tk, tv;
-  tk.init(lds_base(smem), w, l, 2 * VK.sn, kBlk);
-  tv.init(lds_base(smem), w, l, 2 * VV.sn, kBlk);
-  constexpr int IPW = RunLoader<D>::IPW, QSLOT = 3 * Lds::TILE;
-  const int qr = T::RPI * w + l / T::CPR, chunk = ((l % T::CPR) ^ swz<D>(qr)) << 4;   // (Q: 16 rows or a multiple of it further
-  const unsigned ldsq = lds_base(smem) + QSLOT + wave_uniform(w) * 1024;              // with each load: the same swizzle)
-  // Loads of the tile's rows, and of the first two key tiles of a head, need no lengths: they are requested while the lengths
-  // are on their way.  Rows behind a sequence's queries come in like others (their results stay in their lanes and are
-  // written as zeros), and so do keys behind its length (their scores are replaced); rows of V behind it read as zeros.
-  // (2 x 12 heads x 512 tiles of 8 and 2 key tiles: 240 -> XX us.)
-  auto rsrc = [&](const View& v, int keys) {
-    return tile_rsrc(reinterpret_cast<const bf16*>(v.p) + x.key_at(v), (keys - 1) * 2 * v.sn + 2 * D);
-  };
-  BufDesc descK;
-  if constexpr (!PART) {
-    x.t0 = 0;
-    if (!pt.packed) {
-      const bf16* q = reinterpret_cast<const bf16*>(a.Q.p) + x.at(a.Q, RowOf{x.ub, 0, x.r0, true});
-      const BufDesc dq = tile_rsrc(q, (min(kBlk, a.Nq - x.r0) - 1) * 2 * a.Q.sn + 2 * D);
-#pragma unroll
-      for (int k = 0; k < IPW; ++k) load_to_lds16(dq, (qr + 4 * T::RPI * k) * 2 * a.Q.sn + chunk, 0, ldsq + 4096 * k);
-    }
-    descK = rsrc(VK, max(a.Nk, 1));
-    if (a.Nk > 0) tk.template load<0>(descK, 0);
-    if (a.Nk > kBlk) tk.template load<2 * Lds::TILE>(descK, tk.tile_step);
-  }
-  x.template range<PART>(a, pt);
   const int steps = x.steps, h0 = x.h0;
-  const BufDesc descV = rsrc(VV, x.keys());   // (up to the last valid one of this workgroup)
-  if constexpr (PART) {
-    descK = rsrc(VK, x.keys());
-    if (steps > 0) tk.template load<0>(descK, 0);
-    if (steps > 1) tk.template load<2 * Lds::TILE>(descK, tk.tile_step);
-  }
-  if (steps > 0) tv.template load<Lds::TILE>(descV, 0);
   const RowOf row = x.row(a, pt, qh * 32 + ln);   // this lane's
   const RowKeys rk = row_keys(a, x, row);
   const bool live = rk.live;
@@ -99,19 +64,36 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
       bias[i] = table_at(a, bucket_of(a.bias, i - hg * width - far - kBiasPad), h0 + hg) * kLog2e;
     }
   }
-  if (PART || pt.packed) {
-    __syncthreads();
-    const BufDesc dq = tile_rsrc(reinterpret_cast<const bf16*>(a.Q.p) + qbase, 0x7fff0000);
-#pragma unroll
-    for (int k = 0; k < IPW; ++k) {
-      const int o = rowq[qr + 4 * T::RPI * k];
-      load_to_lds16(dq, o < 0 ? (int)kPastEnd : o + chunk, 0, ldsq + 4096 * k);
-    }
-  }
+  __syncthreads();
+
   f32x16 oT[NT];
 #pragma unroll
   for (int et = 0; et < NT; ++et) oT[et] = zero_f32x16();
   float m = -INFINITY, lsum = 0.0f;
+  const View &VK = x.pre ? a.Kp : a.K, &VV = x.pre ? a.Vp : a.V;
+  RunLoader<D> tk, tv;
+  tk.init(lds_base(smem), w, l, 2 * VK.sn, kBlk);
+  tv.init(lds_base(smem), w, l, 2 * VV.sn, kBlk);
+  constexpr int IPW = RunLoader<D>::IPW, QSLOT = 3 * Lds::TILE;
+  // the descriptors span this workgroup's keys up to the last valid one: rows behind it read as zeros
+  auto rsrc = [&](const View& v) {
+    return tile_rsrc(reinterpret_cast<const bf16*>(v.p) + x.key_at(v), (x.keys() - 1) * 2 * v.sn + 2 * D);
+  };
+  const BufDesc descK = rsrc(VK), descV = rsrc(VV);
+  {
+    const BufDesc dq = tile_rsrc(reinterpret_cast<const bf16*>(a.Q.p) + qbase, 0x7fff0000);
+    const int qr = T::RPI * w + l / T::CPR, chunk = ((l % T::CPR) ^ swz<D>(qr)) << 4;
+#pragma unroll
+    for (int k = 0; k < IPW; ++k) {   // (16 rows or a multiple of it further each time: the same swizzle)
+      const int o = rowq[qr + 4 * T::RPI * k];
+      load_to_lds16(dq, o < 0 ? (int)kPastEnd : o + chunk, 0, lds_base(smem) + QSLOT + wave_uniform(w) * 1024 + 4096 * k);
+    }
+  }
+  if (steps > 0) {
+    tk.template load<0>(descK, 0);
+    tv.template load<Lds::TILE>(descV, 0);
+    if (steps > 1) tk.template load<2 * Lds::TILE>(descK, tk.tile_step);
+  }
   // per-lane LDS offsets of the operand reads inside a tile; accumulator tile et holds feature tile et ^ rot: the half
   // of the features that the wave finishes by itself comes first
   const int rot = wave_uniform(par) * HT;
@@ -137,7 +119,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   // The scores of a step are formed one step ahead: their products run under the exponentials of the current step.
   f32x16 sT = zero_f32x16();
   bf16x8 qf[KT], k0[KT];
-  if (!PART && !pt.packed && steps > 1) wait_vm<2 * IPW>();   // Q and K_0 have landed; K_1 and V_0 may stay in flight
+  if (steps > 1) wait_vm<2 * IPW>();   // Q and K_0 have landed; V_0 and K_1 may stay in flight
   else wait_vm0();
   __syncthreads();
   {

@@ -22,7 +22,7 @@ struct FwdTile {
   int limmax;            // keys that any of the rows may see
   int t0, steps;         // first key tile of this part, number of them
 
-  // the place, from the launch alone; false: nothing to do
+  // false: nothing to do
   template <bool PART>
   __device__ __forceinline__ bool open(const Attn& a, const AttnPlan& plan) {
     pre = PART && (int)blockIdx.x < plan.prefix.blocks;
@@ -47,11 +47,6 @@ struct FwdTile {
     h0 = (pre ? unit : unit - ub * per_b) * pt.heads;
     hk = h0 / a.G;
     r0 = tile * kBlk;
-    return true;
-  }
-  // the keys, which depend on the lengths
-  template <bool PART>
-  __device__ __forceinline__ void range(const Attn& a, const AttnPart& pt) {
     if (pre) {
       limmax = a.Np;
     } else {
@@ -64,6 +59,7 @@ struct FwdTile {
     t0 = PART ? (int)((long long)T_all * part / pt.splits) : 0;
     const int t1 = PART ? (int)((long long)T_all * (part + 1) / pt.splits) : T_all;
     steps = wave_uniform(t1 - t0);
+    return true;
   }
   __device__ __forceinline__ RowOf row(const Attn& a, const AttnPart& pt, int i) const {   // i: 0 .. 63
     RowOf o;
