@@ -149,7 +149,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   const float cs = BIAS ? 1.0f : c2;              // the scores' factor in the exponent of 2
   const float* const brow = bias + (BIAS ? row.g * width + far + kBiasPad : 0);   // at distance 0
   int key0 = x.t0 * kBlk + 32 * wave_uniform(par);  // first key of this wave in the current tile
-  int koff = 3 * tk.tile_step, voff = 2 * tv.tile_step;
+  unsigned koff = 3u * (unsigned)tk.tile_step, voff = 2u * (unsigned)tv.tile_step;
   // One step; P = parity of s.  On entry K_{s+1} and V_s are in their slots for every wave and sT holds S_s; sN
   // receives S_{s+1}.  The wave copies its operands to registers first; a second barrier then frees both slots for
   // K_{s+3} and V_{s+2}.  MID: s + 3 < steps, where every condition holds.
@@ -196,19 +196,18 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
     // of 1), so that the accumulators are rescaled on few steps.
     constexpr float kLazy = 8.0f;
     if (__any((mnew - m) * cs > kLazy)) {
-      const float alpha = fast_exp2((m - mnew) * cs);
-      const bool first = m == -INFINITY;   // (also where mnew is: no key yet)
-      lsum = first ? 0.0f : lsum * alpha;
+      const float alpha = mnew == -INFINITY ? 1.0f : fast_exp2((m - mnew) * cs);   // (no key yet: nothing to scale)
+      lsum *= alpha;
 #pragma unroll
       for (int et = 0; et < NT; ++et)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) oT[et][r] = first ? 0.0f : oT[et][r] * alpha;
+        for (int r = 0; r < 16; ++r) oT[et][r] *= alpha;
       m = mnew;
     }
     const float moff = m == -INFINITY ? 0.0f : -m * cs;
     __syncthreads();   // every wave holds its operands of this step: both slots are refilled
-    if (MID || s + 3 < steps) tk.template load<KN>(descK, koff);
-    if (MID || s + 2 < steps) tv.template load<VS>(descV, voff);
+    if (MID || s + 3 < steps) tk.template load<KN>(descK, (int)koff);
+    if (MID || s + 2 < steps) tv.template load<VS>(descV, (int)voff);
     koff += tk.tile_step;
     voff += tv.tile_step;
     key0 += kBlk;
@@ -266,7 +265,8 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(Attn a, AttnPlan plan,
   const float m_o = ml[(((par ^ 1) * 2 + qh) * 32 + ln) * 2 + 0];
   const float l_o = ml[(((par ^ 1) * 2 + qh) * 32 + ln) * 2 + 1];
   const float mstar = fmaxf(m, m_o);
-  const bool some = mstar != -INFINITY && live;       // the row has seen a key
+  // the row has seen a key, or scores that are no numbers, which a maximum passes over
+  const bool some = live && (mstar != -INFINITY || __builtin_isnan(lsum + l_o));
   const float a_me = some ? fast_exp2((m - mstar) * cs) : 0.0f, a_ot = some ? fast_exp2((m_o - mstar) * cs) : 0.0f;
   const float ltot = lsum * a_me + l_o * a_ot;
   const float cw = PART ? a_me : some ? a_me / ltot : 0.0f;

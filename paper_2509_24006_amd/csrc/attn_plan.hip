@@ -74,6 +74,7 @@ bool attn_forward_fits(const Attn& a) {
   const long long T = ceil_div(a.Nk, kBlk), Tp = ceil_div(a.Np, kBlk);
   if (span(a.K, a.Nk, T, p.own.splits) >= lim || span(a.V, a.Nk, T, p.own.splits) >= lim) return false;
   if (a.Np && (span(a.Kp, a.Np, Tp, p.prefix.splits) >= lim || span(a.Vp, a.Np, Tp, p.prefix.splits) >= lim)) return false;
+  if ((long long)(a.Np ? a.B : 1) * p.own.heads * a.Nq >= lim) return false;   // rows of a unit
   // rows of a packed unit (those of one head are counted from their tile)
   if (p.own.packed || a.Np) {
     auto rows = [&](const View& v) { return ((a.Np ? a.B - 1 : 0) * v.sb + (p.own.heads - 1) * v.sh + (long long)(a.Nq - 1) * v.sn + a.d) * esz; };
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a, AttnPlan plan) {
   float M = -INFINITY;
   for (int i = l; i < total; i += 64) {
     const float2 x = *reinterpret_cast<const float2*>(plan.stat + 2 * at(i));
-    if (x.y > 0.0f) M = fmaxf(M, x.x);
+    if (x.y != 0.0f) M = fmaxf(M, x.x);
   }
 #pragma unroll
   for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a, AttnPlan plan) {
   for (int i0 = 0; i0 < total; i0 += 64) {
     float2 x = {0.0f, 0.0f};
     if (i0 + l < total) x = *reinterpret_cast<const float2*>(plan.stat + 2 * at(i0 + l));
-    const float wt = x.y > 0.0f ? fast_exp2(x.x - M) : 0.0f;
+    const float wt = x.y != 0.0f ? fast_exp2(x.x - M) : 0.0f;   // (a sum that is no number stays one)
     float s = wt * x.y;
 #pragma unroll
     for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
@@ -156,11 +157,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(Attn a, AttnPlan plan) {
       for (int e = 0; e < D / 64; ++e) acc[e] += red[w + x][(D / 64) * l + e];
   }
   if (!in) return;
-  const float inv = lsum > 0.0f ? 1.0f / lsum : 0.0f;
+  const float inv = lsum != 0.0f ? 1.0f / lsum : 0.0f;
   E* o = reinterpret_cast<E*>(a.O.p) + b * a.O.sb + h * a.O.sh + (long long)n * a.O.sn + (D / 64) * l;
   if constexpr (D == 128) put_pair(o, acc[0] * inv, acc[1] * inv);
   else put_one(o, acc[0] * inv);
-  if (a.L && l == 0) a.L[row] = lsum > 0.0f ? M * kLn2 + logf(lsum) : -INFINITY;
+  if (a.L && l == 0) a.L[row] = lsum != 0.0f ? M * kLn2 + logf(lsum) : -INFINITY;
 }
 
 template <class E, int D>

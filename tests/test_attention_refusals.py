@@ -100,6 +100,7 @@ def test_offsets_past_32_bits_are_refused():
     far = dict(sn=1 << 12)                                                            # rows 8 KB apart
     assert _call(_params(B=1, H=8, Hkv=8, Nq=1 << 15, Nk=1 << 19), bytes=BIG, K=far) == -2   # a head of 4 GB through one workgroup
     assert _call(_params(B=1 << 12, H=1, Hkv=1, Nq=1, Nk=1, Np=5), bytes=BIG, Kp=dict(), Vp=dict(), Q=dict(sb=1 << 19)) == -2
+    assert _call(_params(B=1 << 10, H=32, Hkv=1, Nq=1 << 17, Nk=1, Np=5), bytes=BIG, Kp=dict(), Vp=dict(), Q=dict(sb=0, sh=0), O=dict(sb=0, sh=0)) == -2
 
 
 def test_binding_refuses_wrong_tensors():

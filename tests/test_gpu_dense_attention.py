@@ -170,6 +170,57 @@ def test_table_entries_that_hide_their_pairs(dt, low, causal):
 
 
 @pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("borders,two", [([5, 1024], False), ([1, 2, 1000, 1024], True), ([], False), ([], True), ([40, 40], False)])
+def test_borders_of_ones_own(dt, borders, two):
+    nb = (len(borders) + 1) * (2 if two else 1)
+    bk = sla.sla_buckets(nb, int(two), (sla.ctypes.c_int32 * 63)(*borders))
+    for Nq, Nk, d, causal in ((70, 1500, 64, True), (1500, 130, 128, False)):
+        Q, K, V, dO = tensors(dt, 1, 2, 1, Nq, Nk, d)
+        table = torch.randn(nb, 2, device="cuda").to(dt)
+        want = ref.attention(Q, K, V, d ** -0.5, causal, pos=[Nk - Nq], table=table, borders=borders, two_sided=two, dO=dO, result=dt)
+        leaves = [t.clone().requires_grad_(True) for t in (Q, K, V, table)]
+        O = attn.dense_attention(*leaves[:3], causal=causal, table=leaves[3], buckets=bk)
+        within(O, want["O"], "O")
+        for name, got in zip(("dQ", "dK", "dV", "dtable"), torch.autograd.grad(O, leaves, dO)):
+            within(got, want[name], name)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+def test_positions_from_the_end_have_gradients_too(dt):
+    B, H, Hkv, Nq, Nk, d = 3, 4, 2, 70, 200, 64
+    Q, K, V, dO = tensors(dt, B, H, Hkv, Nq, Nk, d)
+    lens = [200, 90, 40]              # (the third: its first queries come before its first key)
+    p = sla.make_attn_params(B, H, Hkv, Nq, Nk, d, dt, True, q_pos=-Nq, q_from_end=True)
+    O, L = sla.sla_attn_forward(p, Q, K, V, k_len=ints(lens))
+    got = sla.sla_attn_backward(p, Q, K, V, O, dO, L, k_len=ints(lens))
+    want = ref.attention(Q, K, V, d ** -0.5, True, None, lens, [n - Nq for n in lens], dO=dO, result=dt)
+    within(O, want["O"], "O")
+    within(L, want["L"], "L")
+    for name, x in zip(("dQ", "dK", "dV"), got):
+        within(x, want[name], name)
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("Nq", [2, 100])
+def test_what_is_no_number_comes_back_as_none(dt, Nq):
+    # a row of Q, a valid row of K, a valid row of V: never a number that hides it
+    Q, K, V, _ = tensors(dt, 1, 2, 2, Nq, 300, 64)
+    good = attn.dense_attention(Q, K, V)
+    bad = Q.clone()
+    bad[0, 1, 1, 3] = math.nan
+    O = attn.dense_attention(bad, K, V)
+    assert bool(torch.isnan(O[0, 1, 1]).all())
+    O[0, 1, 1] = good[0, 1, 1]
+    assert torch.equal(O, good)
+    for t, rows in ((K, [0]), (K, [299]), (K, range(64)), (V, [70])):
+        hurt = t.clone()
+        for r in rows:
+            hurt[0, 0, r] = math.nan
+        O = attn.dense_attention(Q, hurt if t is K else K, hurt if t is V else V)
+        assert bool(torch.isnan(O[0, 0]).all()) and torch.equal(O[0, 1], good[0, 1])
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
 def test_no_keys_at_all(dt):
     Q, K, V, dO = tensors(dt, 2, 4, 2, 70, 0, 64)
     table, bk = torch.randn(8, 4, device="cuda"), sla.position_buckets(8, 20)
