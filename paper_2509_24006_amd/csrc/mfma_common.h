@@ -173,11 +173,13 @@ struct SwzTile {
   static constexpr int IPW = kBlk / RPI / 4;    // loads per wave (4 waves share a tile)
 };
 
+// Rows of 64 features take half of the banks each, neighbours opposite halves, so there rows two apart must not meet: swz(r) =
+// 4 ((r / 2) % 2) + (r / 4) % 4.  (With the other bit, r % 2, a third to a half of the LDS cycles of the d = 64 kernels were
+// conflicts; 256 heads x 1024 with every key, forward / query side / key side, 114 / 137 / 190 -> 108 / 133 / 179 us.)
 template <int D>
 __device__ __forceinline__ int swz(int row) {
-  return (((row & 3) << 2) | ((row >> 2) & 3)) & (D / 8 - 1);
+  return D == 64 ? ((row & 2) << 1) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
 }
-
 
 // byte offset (inside a tile) of the 16-byte chunk `c` of row `row`
 template <int D>
