@@ -26,6 +26,10 @@ __device__ __forceinline__ KeySteps key_steps(const Attn& a, const Seq& s, int j
   return k;
 }
 
+// A softmax over one key is 1 whatever the score is: nothing flows back through it.  What the formula P (dP - D) leaves of
+// such a row is a rounding, so the query side takes P = 0 there and the key side of a sequence of one key drops dK.
+__device__ __forceinline__ float dk_scale(const Attn& a, const Seq& s) { return s.nk == 1 ? 0.0f : a.scale; }
+
 struct BwdPlan {
   KeyPlan key;
   int shares;          // float: workgroups per query tile

@@ -292,6 +292,7 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
     dsum = both(drow);
     nDq = -dsum;
     drow = 0.0f;
+    if (lim == 1) Lq = INFINITY;   // (a single key, see dk_scale; the other rows of its tile see 64 keys at most)
     issue(0, b0);
   }
   for (int j = 0; j < steps; j += 2) {
@@ -369,14 +370,14 @@ __device__ __forceinline__ f32x4* key_slot(const KeyPlan& kp, size_t slot, int w
 }
 template <int D>
 __device__ __forceinline__ void store_keys(const Attn& a, const AttnGrads& gr, unsigned char* stage, f32x16 (&dvT)[D / 64],
-                                           f32x16 (&dkT)[D / 64], int b, int hk, int j, int kh, int xh, bool ok, int l) {
+                                           f32x16 (&dkT)[D / 64], int b, int hk, int j, int kh, int xh, bool ok, float scale, int l) {
   const int rows = a.Nk - j * kBlk - 32 * kh;
 #pragma unroll
   for (int dt = 0; dt < D / 64; ++dt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       dvT[dt][r] = ok ? dvT[dt][r] : 0.0f;
-      dkT[dt][r] = ok ? dkT[dt][r] * a.scale : 0.0f;
+      dkT[dt][r] = ok ? dkT[dt][r] * scale : 0.0f;
     }
   auto at = [&](const View& v) {
     return reinterpret_cast<bf16*>(v.p) + (size_t)b * v.sb + (size_t)hk * v.sh + (size_t)(j * kBlk + 32 * kh) * v.sn + (D / 2) * xh;
@@ -618,7 +619,7 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dkdv_kerne
     return;
   }
   __syncthreads();   // every wave is done with the tiles
-  store_keys<D>(a, gr, smem + wu * Lds::STG, dvT, dkT, b, hk, j, kh, xh, kok, l);
+  store_keys<D>(a, gr, smem + wu * Lds::STG, dvT, dkT, b, hk, j, kh, xh, kok, dk_scale(a, sq), l);
 }
 
 // dK, dV of the key tiles whose steps were cut: the sums of the pieces in order.  Bound by its traffic.
@@ -660,7 +661,7 @@ __global__ __launch_bounds__(256) void attn_kv_join_kernel(Attn a, AttnGrads gr,
       dkT[dt][r] = s[4 * (HT + dt) + r / 4][r % 4];
     }
   store_keys<D>(a, gr, smem + wave_uniform(w) * DkLds<D>::STG, dvT, dkT, b, hk, j, kh, xh,
-                j * kBlk + kh * 32 + (l & 31) < sq.nk, l);
+                j * kBlk + kh * 32 + (l & 31) < sq.nk, dk_scale(a, sq), l);
 }
 
 template <int D>

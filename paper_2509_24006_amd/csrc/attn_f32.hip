@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256, 2) void attn_f32_dq_kernel(Attn a, AttnGrads g
     if (live && g == 0 && wq == 0) Ds[(size_t)bh * a.Nq + n] = Dr;
   }
   float Lr = live ? a.L[(size_t)bh * a.Nq + n] : 0.0f;
-  if (Lr == -INFINITY) Lr = INFINITY;   // (a row without a key: P = 0)
+  if (Lr == -INFINITY || lim == 1) Lr = INFINITY;   // (P = 0: a row without a key, or with a single one, see dk_scale)
   float* const bias = reinterpret_cast<float*>(smem + 2 * TB);
   const int far = a.bias.far, width = 2 * far + 1;
   float* const dist = bias + width;   // [wave][width], then the far sums of the waves
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(256, 2) void attn_f32_key_kernel(Attn a, AttnGrads 
     oK = row_ptr(gr.dK, b, hk, key);
     oV = row_ptr(gr.dV, b, hk, key);
   }
-  const float scale = st.total > kp.piece ? 1.0f : a.scale;
+  const float scale = st.total > kp.piece ? 1.0f : dk_scale(a, sq);
 #pragma unroll
   for (int m = 0; m < NO; ++m) {
 #pragma unroll
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(256) void attn_f32_kv_join_kernel(Attn a, AttnGrads
     f32x4 s = *reinterpret_cast<const f32x4*>(p);
 #pragma unroll 4
     for (int e = 1; e < np; ++e) s += *reinterpret_cast<const f32x4*>(p + (size_t)e * (2 * kBlk * D));
-    if (row < kBlk) s *= a.scale;
+    if (row < kBlk) s *= dk_scale(a, sq);
     *reinterpret_cast<f32x4*>(row_ptr(row < kBlk ? gr.dK : gr.dV, b, hk, key) + c) = s;
   }
 }

@@ -137,6 +137,28 @@ def test_score_sizes(dt, size, scale):
     check(dt, 1, 2, 1, 150, 170, 64, size=size, scale=scale)
 
 
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Nq,Nk,causal,k_len,bias", [
+    (1, 1, True, None, False), (783, 1, False, None, False), (9000, 1, False, None, False), (130, 1, False, None, True),
+    (300, 90, False, [1, 1], False), (70, 200, False, [1, 0], True)])
+def test_nothing_flows_back_through_a_single_key(dt, d, Nq, Nk, causal, k_len, bias):
+    # its probability is 1 whatever the score: the gradients are zeros, not what rounding leaves of P (dP - D)
+    Q, K, V, dO = tensors(dt, 2, 4, 2, Nq, Nk, d, 5)
+    leaves = [t.requires_grad_(True) for t in (Q, K, V)]
+    more = {}
+    if bias:
+        more = dict(table=torch.randn(8, 4, device="cuda", requires_grad=True), buckets=sla.position_buckets(8, 20, True))
+    O = attn.dense_attention(*leaves, causal=causal, k_len=ints(k_len), **more)
+    dQ, dK, dV, *dt_ = torch.autograd.grad(O, leaves + list(more.values())[:1], dO)
+    for name, x in (("dQ", dQ), ("dK", dK), *(("dtable", x) for x in dt_)):
+        assert not bool(x.any()), (name, x.abs().max())
+    for b, n in enumerate(k_len or [1, 1]):
+        if n:
+            assert torch.equal(O[b], V[b].repeat_interleave(2, 0)[:, :1].expand_as(O[b]))
+    assert bool(dV.any())
+
+
 def test_one_key_takes_everything():
     # scores so far apart that one probability is 1 and the others vanish: later tiles move the maximum far
     Q = torch.zeros(1, 1, 64, 64, device="cuda", dtype=BF)
