@@ -29,11 +29,13 @@ struct FwdTile {
     const AttnPart& pt = pre ? plan.prefix : plan.own;
     part = 0;
     if constexpr (PART) {
-      int x = blockIdx.x - (pre ? 0 : plan.prefix.blocks);
-      part = x % pt.splits;
-      x /= pt.splits;
-      tile = x % pt.tiles;
-      unit = x / pt.tiles;
+      // The row tiles that read the same keys follow each other eight blocks apart: on one XCD, whose L2 fetches them once.
+      // (Prefix of 16384, 32 sequences: 16 heads over 4, two row tiles 19.5 -> 18.8 us; 32 heads of 8 new tokens, sixteen, 120 -> 108.)
+      const int x = blockIdx.x - (pre ? 0 : plan.prefix.blocks), cuts = pt.units * pt.splits;
+      const int first = x / (8 * pt.tiles) * 8, m = min(8, cuts - first), r = x - first * pt.tiles, c = first + r % m;
+      tile = r / m;
+      part = c % pt.splits;
+      unit = c / pt.splits;
     } else {
       const TileOf own = plan.map.at(blockIdx.x);
       if (own.i < 0) return false;
