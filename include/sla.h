@@ -212,7 +212,7 @@ typedef struct sla_attn_params {
   int32_t q_pos;        /* q0(b) = q_pos, or with q_from_end Np + k_len[b] + q_pos (the      */
   int32_t q_from_end;   /* newest Nq tokens of every sequence: q_pos = -Nq)                  */
   int32_t table_dtype;  /* of the bias table and its gradient: SLA_F32 or SLA_BF16           */
-  float scale;          /* of the scores, > 0                                                */
+  float scale;          /* of the scores, > 0; 1e-20 to 1e20 (else SLA_EUNSUPPORTED)         */
   sla_buckets buckets;
 } sla_attn_params;
 

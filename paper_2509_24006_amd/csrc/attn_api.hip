@@ -9,6 +9,7 @@ namespace {
 
 constexpr int kMaxRows = 1 << 28;          // positions and their differences stay far inside an int
 constexpr long long kMaxPitch = 1 << 24;   // bytes between rows: offsets inside a tile of 64 stay below 2^30
+constexpr float kMinScale = 1e-20f;        // L / scale stays a float, and -1e30 scale (an empty row) is far below any exponent
 
 inline bool off(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
@@ -16,6 +17,7 @@ int make_attn(const sla_attn_params* p, Attn* a) {
   if (!p) return SLA_EINVAL;
   if (p->B <= 0 || p->H <= 0 || p->Hkv <= 0 || p->Nq <= 0 || p->Nk < 0 || p->Np < 0 || p->H % p->Hkv) return SLA_EINVAL;
   if (!(p->scale > 0.0f) || !isfinite(p->scale)) return SLA_EINVAL;
+  if (p->scale < kMinScale || p->scale > 1.0f / kMinScale) return SLA_EUNSUPPORTED;
   if (p->d != 64 && p->d != 128) return SLA_EUNSUPPORTED;
   if (p->dtype != SLA_F32 && p->dtype != SLA_BF16) return SLA_EUNSUPPORTED;
   if (p->table_dtype != SLA_F32 && p->table_dtype != SLA_BF16) return SLA_EUNSUPPORTED;

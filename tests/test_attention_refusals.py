@@ -157,3 +157,8 @@ def test_reference_gradients_against_differences():
             diff = (f(*up) - f(*down)) / 2e-5
             assert abs(diff - float((want[name][0] * step).sum())) < 1e-7 * (1 + abs(diff)), name
     assert float(want["O"][0][0, :, :].abs().max()) > 0 and float(want["O"][0][1].abs().max()) == 0
+
+
+@pytest.mark.parametrize("scale,code", [(1e-20, 0), (1e20, 0), (9e-21, -2), (1e-38, -2), (1.1e20, -2), (3e38, -2)])
+def test_scales_beyond_what_the_backward_pass_can_divide_by(scale, code):
+    assert _sizes(_params(scale=scale)) == code

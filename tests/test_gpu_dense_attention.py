@@ -635,3 +635,26 @@ def test_layers_of_a_block_together():
     for t, gr in zip((x, text, W, table), grads):
         assert gr.shape == t.shape and bool(torch.isfinite(gr).all()) and float(gr.abs().max()) > 0
     assert float(grads[1][1, :, 13:].abs().max()) == 0   # what lies behind a text's length has no part in it
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("scale", [1e-20, 1e-9, 1e9])
+def test_empty_rows_at_the_ends_of_the_scales(dt, scale):
+    # the first rows see no key; what their gradient would add is kept out at every scale
+    check(dt, 1, 2, 1, 90, 70, 64, causal=True, scale=scale, size=1.0 if scale < 1 else 1e-4)
+
+
+@pytest.mark.parametrize("B,H,Hkv,Nq,d", [(32, 4, 1, 3, 128), (5, 6, 2, 33, 64), (3, 2, 2, 200, 64)])
+def test_prefix_whose_rows_fill_several_tiles(B, H, Hkv, Nq, d):
+    # row tiles that read the same keys next to each other, in groups of eight cuts and a shorter last one
+    g = torch.Generator("cuda").manual_seed(B)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF)
+    Np, Nk = 1111, Nq + 77
+    k_len = [max(Nq, Nk - 9 * b) for b in range(B)]
+    Q, K, V, Kp, Vp = r(B, H, Nq, d), r(B, Hkv, Nk, d), r(B, Hkv, Nk, d), r(Hkv, Np, d), r(Hkv, Np, d)
+    O = attn.cached_attention(Q, K, V, ints(k_len), (Kp, Vp))
+    for b in range(B):   # every sequence by itself, its keys behind the prefix
+        k = torch.cat([Kp, K[b, :, :k_len[b]]], 1)[None]
+        v = torch.cat([Vp, V[b, :, :k_len[b]]], 1)[None]
+        want = ref.attention(Q[b:b + 1], k, v, d ** -0.5, True, None, None, [Np + k_len[b] - Nq], None, [], False, result=BF)
+        within(O[b:b + 1], want["O"], f"O of {b}")
