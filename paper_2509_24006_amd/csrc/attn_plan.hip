@@ -45,6 +45,22 @@ AttnPlan attn_plan(const Attn& a, char* ws) {
   long long len = std::max(2ll, ceil_div(tiles * T + ptiles * Tp, kSlots));
   while (tiles * ceil_div(T, len) + ptiles * ceil_div(Tp, len) > kSlots && len < std::max(T, Tp)) ++len;
   p.own.splits = (int)std::max(1ll, std::min(ceil_div(T, len), 256ll));
+  // Under a causal mask row tiles have from few steps to T of them, and the longest parts decide: cut finer, down to where the load
+  // of a workgroup's place is more than a part.  The load in steps has a part's costs beside its own (as on the key side, see
+  // attn_bwd_plan).  Float, d = 128: 9 heads of 1692 122 -> 105 us, 4 of 2900 152 -> 102.  Rows that were whole stay so: two parts gain
+  // less than the joining launch takes (bf16, 8 heads of 4000 56 -> 54 + 30, float, 16 of 1500 151 -> 137 + 24).
+  if (a.causal && !packed && !a.Np && p.own.splits > 1) {
+    const double load = T - 0.5 * std::min(T, (long long)p.own.tiles);
+    double best = 1e300;
+    for (int n = 2; n <= 16 && 2 * n <= T; ++n) {
+      const double extra = (0.5 * n + 0.5) * (a.dtype == SLA_F32 ? 4.0 : 10.0);
+      const double t = std::max((double)ceil_div(T, n), tiles * (load + extra) / kSlots);
+      if (t < 0.95 * best) {
+        best = t;
+        p.own.splits = n;
+      }
+    }
+  }
   p.prefix.splits = (int)std::max(1ll, std::min(ceil_div(Tp, len), 256ll));
   p.parts = a.Np > 0 || p.own.splits > 1;
   p.map = tile_map(a, p.own.units, p.own.tiles);
@@ -199,7 +215,10 @@ BwdPlan attn_bwd_plan(const Attn& a, char* ws) {
   const int qtiles = (a.Nq + kBlk - 1) / kBlk;
   // float query side: as many parts of a tile as fill the chip's 512 places
   const long long qunits = (long long)a.B * a.H * qtiles;
-  p.shares = !f32 || qunits > 256 ? 1 : qunits > 128 ? 2 : 4;
+  // (under a causal mask half of the steps are empty and the longest rows decide, twice as many places count: d = 128, 9 heads of 1692
+  // 140 -> 111 us, 16 of 1500 206 -> 139)
+  const long long places = a.causal ? 512 : 256;
+  p.shares = !f32 || qunits > places ? 1 : qunits > places / 2 ? 2 : 4;
   p.qparts = (a.Nq + kBlk / p.shares - 1) / (kBlk / p.shares);
   p.map = tile_map(a, a.B * a.H, p.qparts);
   KeyPlan& k = p.key;

@@ -42,6 +42,7 @@ struct FwdTile {
       unit = own.bh;
       tile = a.causal ? plan.own.tiles - 1 - own.i : own.i;   // (longest rows first)
     }
+    if (PART && a.causal && !pt.packed) tile = pt.tiles - 1 - tile;   // (longest rows first)
     unit = wave_uniform(unit);
     tile = wave_uniform(tile);
     const int per_b = a.H / pt.heads;   // units per sequence (prefix: units in all)
