@@ -501,7 +501,7 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dkdv_kerne
     // L and D of this step's 64 queries are requested ahead of the next pair's tiles (loads return in order) and picked
     // up after the first products.  They go global -> LDS into the first KB of this wave's own part of the exchange
     // area, which it overwrites with P and dS only after it has read them back.  Rows past the end read as 0; their Q
-    // and dO rows are zero too, so the finite P they get adds nothing.
+    // and dO rows are zero too, so the finite P they get adds nothing (with a bias: P = 0).
     load_to_lds16(descS, lane_id() * 16, ci * (kBlk * 16), xstat);
     const int qt = ci;
     // (the last step requests its own pair once more, into the other buffer, where nobody reads it: every step then
@@ -560,6 +560,13 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dkdv_kerne
         const float bc = bmid[e0 < 0 ? -far : far];
 #pragma unroll
         for (int r = 0; r < 16; ++r) sm[r] = fast_exp2(fmaf(sm[r], sl2, bc));
+      }
+      int last = sq.nq - qt * kBlk - 32 * xh;   // rows past the end: a large bias may be infinity there
+      if (last < 32) {
+        asm volatile("" : "+v"(last));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (c_row(r, g) >= last) sm[r] = 0.0f;
       }
     } else {
 #pragma unroll

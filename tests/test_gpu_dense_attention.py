@@ -658,3 +658,28 @@ def test_prefix_whose_rows_fill_several_tiles(B, H, Hkv, Nq, d):
         v = torch.cat([Vp, V[b, :, :k_len[b]]], 1)[None]
         want = ref.attention(Q[b:b + 1], k, v, d ** -0.5, True, None, None, [Np + k_len[b] - Nq], None, [], False, result=BF)
         within(O[b:b + 1], want["O"], f"O of {b}")
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("shift", [200.0, -200.0, 3000.0])
+@pytest.mark.parametrize("N,lens,causal", [(100, None, False), (130, [130, 37], False), (200, [70, 200], True)])
+def test_tables_far_from_zero(dt, d, shift, N, lens, causal):
+    # a shift of all entries changes nothing but L: no row of a tile that lies behind the last one may see an exponential of it
+    Q, K, V, dO = tensors(dt, 2, 2, 1, N, N, d, 9)
+    buckets = sla.position_buckets(8, 20, not causal)
+    leaves = [t.requires_grad_(True) for t in (Q, K, V)]
+    table = torch.zeros(8, 2, device="cuda")
+    table[3] = 1.0
+    got = []
+    for s in (0.0, shift):
+        tl = (table + s).requires_grad_(True)
+        O = attn.dense_attention(*leaves, causal=causal, q_len=ints(lens), k_len=ints(lens), table=tl, buckets=buckets)
+        got.append((O, *torch.autograd.grad(O, leaves + [tl], dO)))
+    # float scores around the shift are off by half a step of it (here times 1.5: multiplied by log2 e), twice (score and L);
+    # what a probability's relative error e does to O and the gradients is at most e times the sum of their terms' magnitudes,
+    # which a relative bound of 64 e of the largest element covers with room (the terms are below 16 times it)
+    e = 2 * 1.5 * abs(shift) * 2.0 ** -23 * 64 + (2.0 ** -6 if dt == BF else 2.0 ** -14)
+    for name, x, y in zip(("O", "dQ", "dK", "dV", "dtable"), *got):
+        assert bool(y.isfinite().all()), name
+        assert float((x.double() - y.double()).abs().max()) <= e * float(x.double().abs().max()), name
