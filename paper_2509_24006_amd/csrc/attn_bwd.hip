@@ -170,12 +170,15 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
   auto step = [&](auto Main, int j, auto Buf) __attribute__((always_inline)) {
     constexpr bool MAIN = decltype(Main)::value;
     constexpr int buf = decltype(Buf)::value, KO = buf * Lds::BUF, VO = KO + Lds::TILE;
+    // (registers: with a bias and 128 features K_j^T comes after the table's sums, and fewer operands run ahead; left as in the
+    // other kernels 43 of them spill: 12 heads of 4000 269 -> 194 us, causal 131 -> 102)
+    constexpr bool LATE = BIAS && D == 128;
     const int key0 = j * kBlk + 32 * wave_uniform(kh);
     ad.refresh();
     wait_vm0();
     __syncthreads();   // tiles of step j have landed for every wave; step j - 1 is fully consumed
     if (j + 1 < steps) issue(j + 1, std::integral_constant<int, buf ^ 1>());
-    constexpr int PF = 4;   // LDS reads run PF operand pairs ahead of the products
+    constexpr int PF = LATE ? 3 : 4;   // LDS reads run PF operand pairs ahead of the products
     bf16x8 ka[PF], va[PF], ta[2][NT];
     auto read_s = [&](int t) __attribute__((always_inline)) {
       ka[t % PF] = lds_row(smem, ad.row(t) + KO);
@@ -195,13 +198,14 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
       sched_fence();
     }
     // K_j^T for the third product arrives under the exponentials
-    if constexpr (MAIN) {
+    auto read_k = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int dt = 0; dt < NT; ++dt)
           ta[u][dt] = lds_tr<D>(smem, ad.tr(0, dt) + KO + u * RB, ad.tr(1, dt) + KO + u * RB);
-    }
+    };
+    if constexpr (MAIN && !LATE) read_k();
     sched_fence();
     const int d0 = key0 - pos;   // distance of this wave's first key
     bool near = false;
@@ -268,6 +272,7 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
         pR += d0 < 0 ? 0.0f : ps;
       }
     }
+    if constexpr (LATE) read_k();
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const bf16x8 sb = c_to_operand(dpT, u);
@@ -386,8 +391,9 @@ __device__ __forceinline__ void store_keys(const Attn& a, const AttnGrads& gr, u
   store_rows_bf16<D / 64>(stage, dkT, at(gr.dK), gr.dK.sn, rows, l);
 }
 
+// (d = 64 with a bias: 19 registers spill at three workgroups per CU, and still 157 -> 136 us at 12 heads of 4000)
 template <int D, bool BIAS>
-__global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dkdv_kernel(Attn a, AttnGrads gr, const RowStat* __restrict__ stats, KeyPlan kp,
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_dkdv_kernel(Attn a, AttnGrads gr, const RowStat* __restrict__ stats, KeyPlan kp,
                                                             const float* __restrict__ tpart, int qparts) {
   using Lds = DkLds<D>;
   using T = SwzTile<D>;
