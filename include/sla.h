@@ -191,7 +191,7 @@ int sla_aggregate_states(const sla_params* p, int method, const void* luts, cons
  * 0 .. Np - 1, and behind it the sequence's own first k_len[b] rows, at positions Np ...  A key is allowed where it
  * exists and, with `causal`, kp <= n + q0(b).  Queries n >= q_len[b] and those without an allowed key are empty rows:
  * O = 0, L = -inf, no gradients.  Rows of Q and dO behind q_len[b], and of K and V behind k_len[b], are not read; those
- * of dQ, dK, dV are written as zeros.  (Keys that only `causal` hides have to be finite: they meet a probability of
+ * of dQ, dK, dV are written as zeros.  (Keys that only `causal` or the table hides have to be finite: they meet a probability of
  * zero in a product.) */
 
 /* Buckets of the distance r = kp - (n + q0(b)).  With m = |r| (two_sided) or max(-r, 0): bucket = number of borders
