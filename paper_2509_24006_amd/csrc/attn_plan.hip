@@ -230,7 +230,7 @@ BwdPlan attn_bwd_plan(const Attn& a, char* ws) {
   const double slots = !f32 && a.d == 64 ? 768 : 512, wgs = (double)units * k.quarters, steps = (double)a.G * qtiles;
   double best = 1e300;
   k.pieces = 1;
-  for (int n = 1; n <= 64 && n <= steps; ++n) {
+  for (int n = 1; n <= 64 && n <= steps && k.tiles > 0; ++n) {   // (without keys there is nothing to cut, nor to join)
     const double len = ceil(steps / n), extra = n == 1 ? 3.0 : f32 ? 4.0 : 10.0;
     const double t = a.causal ? (0.5 * wgs * steps + (n > 1 ? 0.5 * n + 0.5 : 1.0) * wgs * extra) / slots + len
                               : ceil(wgs * n / slots) * (len + extra);

@@ -683,3 +683,17 @@ def test_tables_far_from_zero(dt, d, shift, N, lens, causal):
     for name, x, y in zip(("O", "dQ", "dK", "dV", "dtable"), *got):
         assert bool(y.isfinite().all()), name
         assert float((x.double() - y.double()).abs().max()) <= e * float(x.double().abs().max()), name
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("H,Hkv,Nq,d", [(4, 2, 70, 64), (4, 1, 300, 128), (2, 2, 1, 64)])
+def test_no_keys_at_all_under_a_causal_mask(dt, H, Hkv, Nq, d):
+    Q, K, V, dO = tensors(dt, 2, H, Hkv, Nq, 0, d)
+    table, bk = torch.randn(8, H, device="cuda"), sla.position_buckets(8, 20, False)
+    for more in ({}, dict(table=table.clone().requires_grad_(True), buckets=bk)):
+        leaves = [t.clone().requires_grad_(True) for t in (Q, K, V)] + [t for t in list(more.values())[:1]]
+        O = attn.dense_attention(*leaves[:3], causal=True, **more)
+        got = torch.autograd.grad(O, leaves, dO)
+        assert not bool(O.detach().any()) and not bool(got[0].any())
+        assert got[1].shape == K.shape and got[2].shape == V.shape
+        assert not more or not bool(got[3].any())
