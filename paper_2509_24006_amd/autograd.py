@@ -109,7 +109,7 @@ def _laid_out(t: torch.Tensor, token_major: bool) -> torch.Tensor:
     for i in range(t.dim() - 1):
         if n[i] > 1:
             fits = fits and s[i] % q == 0 and (i != rows or n[-1] <= s[i] <= (1 << 24) // t.element_size())
-    return t if fits else t.contiguous()
+    return t if fits else t.clone(memory_format=torch.contiguous_format)   # (contiguous() would hand back a tensor at an odd address)
 
 
 def _attn_params(Q, K, causal, scale, table, buckets, token_major, prefix_rows=0, from_end=False):

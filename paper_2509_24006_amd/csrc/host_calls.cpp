@@ -418,7 +418,7 @@ struct DenseAttention : torch::autograd::Function<DenseAttention> {
       };
       const int64_t esz = dO.element_size();
       if (!c.rows(&dO, p.H, p.Nq, &go) || !whole(go, esz) || go.stride_n < p.d) {
-        dO = dO.contiguous();
+        dO = dO.clone(at::MemoryFormat::Contiguous);   // (contiguous() would hand back a tensor at an odd address)
         TORCH_CHECK(c.rows(&dO, p.H, p.Nq, &go), "dense_attention: the output's gradient has another type or shape");
       }
       TORCH_CHECK(opened && c.rows(&Q, p.H, p.Nq, &q) && c.rows(&K, p.Hkv, p.Nk, &k) && c.rows(&V, p.Hkv, p.Nk, &v) &&

@@ -162,3 +162,18 @@ def test_reference_gradients_against_differences():
 @pytest.mark.parametrize("scale,code", [(1e-20, 0), (1e20, 0), (9e-21, -2), (1e-38, -2), (1.1e20, -2), (3e38, -2)])
 def test_scales_beyond_what_the_backward_pass_can_divide_by(scale, code):
     assert _sizes(_params(scale=scale)) == code
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("shape,token", [((2, 3, 5, 64), False), ((2, 5, 3, 64), True), ((3, 5, 64), False)])
+def test_laid_out_moves_what_begins_at_an_odd_address(dt, shape, token):
+    from paper_2509_24006_amd import autograd as attn
+    n = math.prod(shape)
+    room = torch.arange(n + 16, dtype=torch.float32).to(dt)
+    room = room[(-room.data_ptr() // room.element_size()) % (16 // room.element_size()):]   # at a multiple of 16 bytes
+    fits, odd = room[:n].view(shape), room[1:n + 1].view(shape)
+    assert attn._laid_out(fits, token) is fits
+    leaf = odd.detach().requires_grad_(True)
+    got = attn._laid_out(leaf, token)
+    assert got.data_ptr() % 16 == 0 and got.is_contiguous() and torch.equal(got, odd)
+    assert torch.equal(torch.autograd.grad(got, leaf, fits)[0], fits)

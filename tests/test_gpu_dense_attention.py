@@ -697,3 +697,41 @@ def test_no_keys_at_all_under_a_causal_mask(dt, H, Hkv, Nq, d):
         assert not bool(O.detach().any()) and not bool(got[0].any())
         assert got[1].shape == K.shape and got[2].shape == V.shape
         assert not more or not bool(got[3].any())
+
+
+def off_by_one(t):
+    """the same values in a contiguous tensor that begins one element behind a multiple of 16 bytes"""
+    x = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)[1:].view(t.shape)
+    x.copy_(t.detach())
+    assert x.is_contiguous() and x.data_ptr() % 16 == t.element_size()
+    return x
+
+
+@pytest.mark.parametrize("dt", [F32, BF], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("token", [False, True], ids=["head_major", "token_major"])
+def test_contiguous_tensors_at_odd_addresses(dt, token):
+    Q, K, V, dO = tensors(dt, 2, 4, 4, 70, 70, 64)
+    if token:
+        Q, K, V, dO = (t.transpose(1, 2).contiguous() for t in (Q, K, V, dO))
+    new = lambda: [t.clone().requires_grad_(True) for t in (Q, K, V)]
+    plain = new()
+    O = attn.dense_attention(*plain, causal=True, token_major=token)
+    want = (O.detach(),) + torch.autograd.grad(O, plain, dO)
+    for i in range(4):   # Q, K, V, and the incoming gradient by itself
+        ls, go = new(), dO
+        if i < 3:
+            ls[i] = off_by_one(ls[i]).requires_grad_(True)
+        else:
+            go = off_by_one(dO)
+        O = attn.dense_attention(*ls, causal=True, token_major=token)
+        got = (O.detach(),) + torch.autograd.grad(O, ls, go)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+    ls = [off_by_one(t).requires_grad_(True) for t in (Q, K, V)]
+    O = attn.dense_attention(*ls, causal=True, token_major=token)
+    got = (O.detach(),) + torch.autograd.grad(O, ls, off_by_one(dO))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    prefix = tuple(torch.randn((130, 4, 64) if token else (4, 130, 64), device="cuda").to(dt) for _ in range(2))
+    want = attn.cached_attention(Q, K, V, prefix=prefix, token_major=token)
+    got = attn.cached_attention(off_by_one(Q), off_by_one(K), off_by_one(V), prefix=tuple(off_by_one(t) for t in prefix),
+                                token_major=token)
+    assert torch.equal(got, want)
