@@ -20,6 +20,7 @@ from __future__ import annotations
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as sla
 from .binding import position_buckets  # noqa: F401  (the buckets of dense_attention's and cached_attention's bias)
@@ -96,9 +97,16 @@ class _AttnFunction(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dO):
+        _no_tangents("dense_attention's backward pass", dO)
         Q, K, V, table, O, L, q_len, k_len = ctx.saved_tensors
         grads = sla.sla_attn_backward(ctx.p, Q, K, V, O, _laid_out(dO, ctx.token_major), L, table, q_len, k_len, ctx.token_major)
         return (*grads, None, None, None, None)
+
+
+def _no_tangents(what: str, *tensors):
+    """Refuses inputs of forward-mode differentiation: the kernels would take them for constants."""
+    if any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise sla.SLAError(f"{what} has no forward-mode derivative")
 
 
 def _laid_out(t: torch.Tensor, token_major: bool) -> torch.Tensor:
@@ -144,10 +152,12 @@ def dense_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: b
     keys of every sequence; what lies behind them is not read, and comes back as zeros.  table [n_buckets,H] (float32
     or bf16) with buckets = position_buckets(...): table[bucket(key position - query position), head] is added
     to the scaled scores; an entry of -1e30 or below hides its pairs.  A row that sees no key is zero.  Keys and values that
-    only the causal order or the table hides have to be finite: they meet a probability of zero in a product."""
+    only the causal order or the table hides have to be finite: they meet a probability of zero in a product.
+    Forward-mode differentiation (dual tensors) is refused, here and in cached_attention."""
     O = _attend(Q, K, V, None, table, q_len, k_len, buckets, causal, scale, token_major, False)
     if O is not None:
         return O
+    _no_tangents("dense_attention", Q, K, V, table)
     Q, K, V = (_laid_out(t, token_major) for t in (Q, K, V))
     p = _attn_params(Q, K, causal, scale, table, buckets, token_major)
     if table is not None and not table.is_contiguous():
@@ -170,6 +180,7 @@ def cached_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, k_len: O
     O = _attend(Q, K, V, prefix, table, None, k_len, buckets, causal, scale, token_major, True)
     if O is not None:
         return O
+    _no_tangents("cached_attention", Q, K, V, table, *(prefix or ()))
     with torch.no_grad():
         Q, K, V = (_laid_out(t, token_major) for t in (Q, K, V))
         if prefix is not None:

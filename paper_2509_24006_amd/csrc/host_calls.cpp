@@ -338,6 +338,9 @@ struct Attend {   // what a call is given beside its tensors
   double scale;   // 0: 1 / sqrt(d)
 };
 
+// an input of forward-mode differentiation, which the kernels would take for a constant
+bool tangent(const at::Tensor& t) { return t._fw_grad(0).defined(); }
+
 const at::Tensor* defined(const at::Tensor& t) { return t.defined() ? &t : nullptr; }
 
 bool attend_params(const Attend& a, const at::Tensor& Q, const at::Tensor& K, const at::Tensor* Kp, const at::Tensor* table,
@@ -416,6 +419,7 @@ struct DenseAttention : torch::autograd::Function<DenseAttention> {
         return (reinterpret_cast<uintptr_t>(t.data) | (t.stride_b * esz) | (t.stride_h * esz) | (t.stride_n * esz)) % 16 == 0 &&
                t.stride_n * esz <= 1 << 24;
       };
+      TORCH_CHECK(!tangent(dO), "dense_attention's backward pass has no forward-mode derivative");
       const int64_t esz = dO.element_size();
       if (!c.rows(&dO, p.H, p.Nq, &go) || !whole(go, esz) || go.stride_n < p.d) {
         dO = dO.clone(at::MemoryFormat::Contiguous);   // (contiguous() would hand back a tensor at an odd address)
@@ -464,6 +468,7 @@ PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   for (int i = 0; i < 8; ++i) {
     t[i] = a[i] == Py_None ? nullptr : plain(a[i]);
     if (!t[i] && (a[i] != Py_None || i < 3)) Py_RETURN_NONE;
+    if (t[i] && tangent(*t[i])) Py_RETURN_NONE;   // (refused there)
   }
   const at::Tensor &Q = *t[0], &K = *t[1], &V = *t[2];
   if (!Q.is_cuda() || (t[3] != nullptr) != (t[4] != nullptr)) Py_RETURN_NONE;

@@ -177,3 +177,21 @@ def test_laid_out_moves_what_begins_at_an_odd_address(dt, shape, token):
     got = attn._laid_out(leaf, token)
     assert got.data_ptr() % 16 == 0 and got.is_contiguous() and torch.equal(got, odd)
     assert torch.equal(torch.autograd.grad(got, leaf, fits)[0], fits)
+
+
+def test_forward_mode_is_refused():
+    import torch.autograd.forward_ad as fwd
+    from paper_2509_24006_amd import autograd as attn
+    q, p, t, bk = torch.zeros(1, 2, 3, 64), torch.zeros(2, 3, 64), torch.zeros(8, 2), sla.position_buckets(8, 20)
+    with fwd.dual_level():
+        for i in range(4):
+            a = [q, q, q, t]
+            a[i] = fwd.make_dual(a[i].clone(), torch.ones_like(a[i]))
+            with pytest.raises(sla.SLAError, match="forward-mode"):
+                attn.dense_attention(*a[:3], table=a[3], buckets=bk)
+            with pytest.raises(sla.SLAError, match="forward-mode"):
+                attn.cached_attention(*a[:3], table=a[3], buckets=bk)
+        d = fwd.make_dual(p, torch.ones_like(p))
+        for prefix in ((d, p), (p, d)):
+            with pytest.raises(sla.SLAError, match="forward-mode"):
+                attn.cached_attention(q, q, q, prefix=prefix)

@@ -735,3 +735,41 @@ def test_contiguous_tensors_at_odd_addresses(dt, token):
     got = attn.cached_attention(off_by_one(Q), off_by_one(K), off_by_one(V), prefix=tuple(off_by_one(t) for t in prefix),
                                 token_major=token)
     assert torch.equal(got, want)
+
+
+def test_forward_mode_is_refused():
+    import torch.autograd.forward_ad as fwd
+    Q, K, V, dO = tensors(BF, 2, 4, 2, 30, 40, 64)
+    table, bk, lens = torch.randn(8, 4, device="cuda"), sla.position_buckets(8, 20), ints([40, 7])
+    prefix = tuple(torch.randn(2, 50, 64, device="cuda").to(BF) for _ in range(2))
+    dense = lambda q, k, v, t: attn.dense_attention(q, k, v, k_len=lens, table=t, buckets=bk)
+    cached = lambda q, k, v, t, kp, vp: attn.cached_attention(q, k, v, lens, (kp, vp), table=t, buckets=bk)
+    for call, given in ((dense, (Q, K, V, table)), (cached, (Q, K, V, table, *prefix))):
+        want = call(*given)
+        with fwd.dual_level():
+            for i, t in enumerate(given):
+                for mode in (torch.enable_grad, torch.no_grad):
+                    for other in (False, True):   # beside a leaf whose gradient is wanted
+                        args = list(given)
+                        args[i] = fwd.make_dual(t, torch.ones_like(t))
+                        if other:
+                            args[i - 1] = args[i - 1].clone().requires_grad_(True)
+                        with mode(), pytest.raises(RuntimeError, match="forward-mode"):
+                            call(*args)
+            assert torch.equal(call(*given), want)   # a level alone changes nothing
+        assert torch.equal(call(*given), want)
+
+
+@pytest.mark.parametrize("odd", [False, True], ids=["compiled_node", "python_node"])
+def test_forward_mode_through_the_backward_pass_is_refused(odd):
+    import torch.autograd.forward_ad as fwd
+    Q, K, V, dO = tensors(BF, 2, 4, 2, 30, 40, 64)
+    if odd:
+        Q = torch.zeros(2, 4, 30, 67, device="cuda", dtype=BF)[..., 1:65].copy_(Q)
+    ls = [t.detach().requires_grad_(True) for t in (Q, K, V)]
+    O = attn.dense_attention(*ls)
+    want = torch.autograd.grad(O, ls, dO, retain_graph=True)
+    with fwd.dual_level():
+        with pytest.raises(RuntimeError, match="forward-mode"):
+            torch.autograd.grad(O, ls, fwd.make_dual(dO, torch.ones_like(dO)), retain_graph=True)
+        assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(O, ls, dO), want))
