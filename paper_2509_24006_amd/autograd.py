@@ -103,6 +103,12 @@ class _AttnFunction(torch.autograd.Function):
         return (*grads, None, None, None, None)
 
 
+def _no_trace(what: str):
+    """A trace would record the allocation of the output and nothing that fills it."""
+    if torch.jit.is_tracing():
+        raise sla.SLAError(f"{what} cannot be traced")
+
+
 def _no_tangents(what: str, *tensors):
     """Refuses inputs of forward-mode differentiation: the kernels would take them for constants."""
     if any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
@@ -153,10 +159,11 @@ def dense_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: b
     or bf16) with buckets = position_buckets(...): table[bucket(key position - query position), head] is added
     to the scaled scores; an entry of -1e30 or below hides its pairs.  A row that sees no key is zero.  Keys and values that
     only the causal order or the table hides have to be finite: they meet a probability of zero in a product.
-    Forward-mode differentiation (dual tensors) is refused, here and in cached_attention."""
+    Forward-mode differentiation (dual tensors) and torch.jit.trace are refused, here and in cached_attention."""
     O = _attend(Q, K, V, None, table, q_len, k_len, buckets, causal, scale, token_major, False)
     if O is not None:
         return O
+    _no_trace("dense_attention")
     _no_tangents("dense_attention", Q, K, V, table)
     Q, K, V = (_laid_out(t, token_major) for t in (Q, K, V))
     p = _attn_params(Q, K, causal, scale, table, buckets, token_major)
@@ -180,6 +187,7 @@ def cached_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, k_len: O
     O = _attend(Q, K, V, prefix, table, None, k_len, buckets, causal, scale, token_major, True)
     if O is not None:
         return O
+    _no_trace("cached_attention")
     _no_tangents("cached_attention", Q, K, V, table, *(prefix or ()))
     with torch.no_grad():
         Q, K, V = (_laid_out(t, token_major) for t in (Q, K, V))

@@ -17,6 +17,7 @@
 #include <cstring>
 
 #include <ATen/ATen.h>
+#include <ATen/TracerMode.h>
 #include <c10/core/DeviceGuard.h>
 
 #include "../../include/sla.h"
@@ -463,7 +464,7 @@ struct DenseAttention : torch::autograd::Function<DenseAttention> {
 //        cached) -> O, or None where the Python code has to lay out, check or refuse
 PyObject* attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (n != 13) Py_RETURN_NONE;
+  if (n != 13 || at::tracer::impl::is_dispatch_enabled()) Py_RETURN_NONE;   // (a traced call is refused there)
   const at::Tensor* t[8];
   for (int i = 0; i < 8; ++i) {
     t[i] = a[i] == Py_None ? nullptr : plain(a[i]);

@@ -195,3 +195,11 @@ def test_forward_mode_is_refused():
         for prefix in ((d, p), (p, d)):
             with pytest.raises(sla.SLAError, match="forward-mode"):
                 attn.cached_attention(q, q, q, prefix=prefix)
+
+
+def test_a_traced_call_is_refused():
+    from paper_2509_24006_amd import autograd as attn
+    q = torch.zeros(1, 2, 3, 64)
+    for f in (attn.dense_attention, attn.cached_attention):
+        with pytest.raises(sla.SLAError, match="traced"):
+            torch.jit.trace(lambda x: f(x, x, x), (q,), check_trace=False)

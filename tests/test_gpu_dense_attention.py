@@ -773,3 +773,13 @@ def test_forward_mode_through_the_backward_pass_is_refused(odd):
         with pytest.raises(RuntimeError, match="forward-mode"):
             torch.autograd.grad(O, ls, fwd.make_dual(dO, torch.ones_like(dO)), retain_graph=True)
         assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(O, ls, dO), want))
+
+
+def test_a_traced_call_is_refused():
+    Q, K, V, _ = tensors(BF, 1, 2, 2, 8, 40, 64)
+    want = attn.dense_attention(Q, K, V), attn.cached_attention(Q, K, V)
+    for f in (attn.dense_attention, attn.cached_attention):
+        for leaf in (Q, Q.clone().requires_grad_(True)):
+            with pytest.raises(sla.SLAError, match="traced"):
+                torch.jit.trace(lambda q, k, v: f(q, k, v) * 1, (leaf, K, V), check_trace=False)
+    assert torch.equal(attn.dense_attention(Q, K, V), want[0]) and torch.equal(attn.cached_attention(Q, K, V), want[1])
