@@ -197,7 +197,9 @@ int sla_aggregate_states(const sla_params* p, int method, const void* luts, cons
 /* Buckets of the distance r = kp - (n + q0(b)).  With m = |r| (two_sided) or max(-r, 0): bucket = number of borders
  * <= m, plus n_buckets / 2 where two_sided and r > 0.  n_buckets = 0: no bias.  A side has n_buckets (two_sided:
  * n_buckets / 2) buckets, at most 64, and one border less; borders ascend from 1 at least to SLA_ATTN_MAX_DISTANCE.  Table
- * entries of -1e30 and below hide their pairs: a key that a row sees only through them does not exist for it. */
+ * entries of -1e30 and below hide their pairs: a key that a row sees only through them does not exist for it.  Other
+ * entries are numbers to be added, not masks: scores and L are floats, so a row that sees nothing but entries of magnitude t has
+ * probabilities that are off by a factor of up to about exp(t 2^-21) in the backward pass (0.5 % at t = 1e4; all is lost at 1e8). */
 enum { SLA_ATTN_BORDERS = 63, SLA_ATTN_MAX_DISTANCE = 1024 };
 typedef struct sla_buckets {
   int32_t n_buckets, two_sided;

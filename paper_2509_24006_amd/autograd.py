@@ -157,8 +157,10 @@ def dense_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal: b
     causal: query n sees the keys up to n + Nk - Nq.  q_len, k_len (int32 [B], on the device): valid queries and
     keys of every sequence; what lies behind them is not read, and comes back as zeros.  table [n_buckets,H] (float32
     or bf16) with buckets = position_buckets(...): table[bucket(key position - query position), head] is added
-    to the scaled scores; an entry of -1e30 or below hides its pairs.  A row that sees no key is zero.  Keys and values that
-    only the causal order or the table hides have to be finite: they meet a probability of zero in a product.
+    to the scaled scores; an entry of -1e30 or below hides its pairs, and others should stay below 1e4 in magnitude where a row
+    sees nothing else (its scores and their statistic are floats: the gradients are lost from 1e8 on).  A row that sees no key is
+    zero.  Keys and values that only the causal order or the table hides have to be finite: they meet a probability of zero
+    in a product.
     Forward-mode differentiation (dual tensors) and torch.jit.trace are refused, here and in cached_attention."""
     O = _attend(Q, K, V, None, table, q_len, k_len, buckets, causal, scale, token_major, False)
     if O is not None:

@@ -45,6 +45,7 @@ __device__ __forceinline__ RowStat row_stat(float L, float D, float rscale) {
 }
 
 // ------------------------------------------------------------------ dQ
+// (d = 128 with a bias: 74804 + 40 far bytes in all, two workgroups per CU up to far = 177 and one beyond.)
 template <int D>
 struct DqLds {
   static constexpr int TILE = SwzTile<D>::BYTES;
@@ -359,6 +360,7 @@ __global__ __launch_bounds__(256, D == 64 && !BIAS ? 3 : 2) void attn_dq_kernel(
 // (a wave issues one in five cycles or more): loads with one M0 a tile, descriptors that change with the head only, L and
 // D as a ready operand.  (Instructions of a step 414 -> 290 at d = 128, 337 -> 240 at d = 64; key side of 256 heads x 1024,
 // d = 64, 221 -> 195 us, of 12 x 32760, d = 128, 12.58 -> 12.19 ms.)
+// LDS at d = 128 is half of a CU's without a bias; any bias beside it leaves one workgroup per CU.
 template <int D>
 struct DkLds {
   static constexpr int TILE = SwzTile<D>::BYTES;

@@ -12,7 +12,9 @@ namespace sla {
 
 namespace {
 
-constexpr int kSlots = 512;   // workgroups that run at a time: two per CU
+// Workgroups that the forward plan has room for: two per CU, as the bf16 kernels run at d = 128 and with a bias.  (Those at d = 64
+// without one run three per CU and the float ones three or four: there keys are cut into fewer parts than would run at a time.)
+constexpr int kSlots = 512;
 
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
@@ -40,7 +42,9 @@ AttnPlan attn_plan(const Attn& a, char* ws) {
   const long long T = ceil_div(a.Nk, kBlk), Tp = ceil_div(a.Np, kBlk);
   if (a.Np > 0) p.prefix = part_of(a.H / heads, heads, (long long)a.B * heads * a.Nq, true);
   // Parts of about equal length, two key tiles or more each (less does not pay for a part's fixed cost and its sums),
-  // as many as run at a time: one more would wait for a whole round.
+  // kSlots of them at most: one more would wait for a whole round.  They are counted by the capacities Nk and Np, and every sequence's own
+  // keys are then cut into as many: from kSlots row tiles on nothing is cut, and a long sequence among short ones is read by one
+  // workgroup per row tile.
   const long long tiles = (long long)p.own.units * p.own.tiles, ptiles = (long long)p.prefix.units * p.prefix.tiles;
   long long len = std::max(2ll, ceil_div(tiles * T + ptiles * Tp, kSlots));
   while (tiles * ceil_div(T, len) + ptiles * ceil_div(Tp, len) > kSlots && len < std::max(T, Tp)) ++len;
@@ -227,6 +231,7 @@ BwdPlan attn_bwd_plan(const Attn& a, char* ws) {
   k.quarters = f32 ? (units < 384 ? 4 : 2) : 1;
   k.map = tile_map(a, a.B * a.Hkv, k.tiles);
   k.blocks = f32 ? (int)units * k.quarters : k.map.blocks();
+  // (workgroups at a time; d = 128 with a bias runs one per CU, see DkLds, and is counted as two)
   const double slots = !f32 && a.d == 64 ? 768 : 512, wgs = (double)units * k.quarters, steps = (double)a.G * qtiles;
   double best = 1e300;
   k.pieces = 1;
